@@ -293,6 +293,106 @@ RBS_API rbs_status rbs_prefill_varlen(int n_prompts, const int* cu_seqlens, int 
                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * What stands around the prefill path in a serving engine: the queries and keys on their way into it, the paged cache
+ * that keeps the keys and values, and the tokens generated from that cache.  (The paper's path begins with Q, K, V that are
+ * already normed and rotated and ends with the prompt; these calls have no counterpart in it.)
+ *
+ * A paged cache is a pair of bf16 tensors (k_cache, v_cache) of n_pages pages of page_size tokens,
+ *     element(page, o, h, j) = ptr[page*stride_batch + o*stride_token + h*stride_head + j],
+ * with any strides that are multiples of 8 (pages that hold token rows, or head rows; the two tensors need not agree).
+ * Token t of sequence s lives at offset t % page_size of page block_table[s*table_stride + t / page_size]; its slot is
+ * page*page_size + offset.  Any page_size >= 1.  A sequence has at most max_pages*page_size tokens.
+ */
+typedef struct {
+  int n_seqs;       /* S, at most 8192 in rbs_paged_extend */
+  int n_q_heads;    /* Hq */
+  int n_kv_heads;   /* Hkv */
+  int head_dim;     /* 128 */
+  int page_size;    /* tokens per page */
+  int n_pages;      /* pages of the cache; n_pages * page_size < 2^31 */
+  int max_pages;    /* entries of a block-table row that belong to the sequence */
+  int table_stride; /* entries from one block-table row to the next, >= max_pages */
+} rbs_paged_shape;
+
+/*
+ * Adds tokens to sequences: sequence s has seq_lens[s] tokens in the cache and gets new_lens[s] more (negative lengths count
+ * as 0, lengths above max_pages*page_size as that).  All arrays are device int32.
+ *   - Pages: sequence s needs ceil(out_lens[s] / page_size) - ceil(seq_lens[s] / page_size) more.  They are taken from
+ *     free_pages in order, sequences in order, from entry free_used[0] on (free_used == NULL: from the first), and written
+ *     to block_table behind the pages that the sequence has; other entries are left as they are.  free_used_out[0] =
+ *     free_used[0] + pages needed.  Where that exceeds n_free the entries without a page are written as -1.
+ *   - Tokens: the new tokens are packed sequence after sequence into n_tokens rows.  cu_new[S + 1]: their prefix sums.
+ *     positions[i], slots[i]: position of row i's token in its sequence, and its slot; slot -1 for a token without one (its
+ *     page lies outside [0, n_pages), or its position is max_pages*page_size or more).  Rows behind the last token get
+ *     position 0 and slot -1.  New tokens that the n_tokens rows cannot hold are not added.
+ *   - out_lens[s] = tokens of the sequence afterwards, at most max_pages*page_size.
+ * n_free and n_tokens may be 0 (their arrays may then be NULL).  The output arrays must not overlap the inputs (out_lens ==
+ * seq_lens and free_used_out == free_used are RBS_ERR_INVALID_ARG): every thread block reads all lengths.  The call does the
+ * same again when repeated; to go on, hand it out_lens and free_used_out.
+ * RBS_ERR_UNSUPPORTED: n_seqs > 8192, max_pages*page_size + n_tokens >= 2^31.  Of the shape, head counts and head_dim are
+ * not looked at.  No workspace.
+ */
+RBS_API rbs_status rbs_paged_extend(const rbs_paged_shape* shape, const int* seq_lens, const int* new_lens,
+                                    const int* free_pages, int n_free, const int* free_used, int n_tokens, int* block_table,
+                                    int* out_lens, int* cu_new, int* positions, int* slots, int* free_used_out,
+                                    void* stream);
+
+/* Norm of each head and rotation by position, for a token at position p (head row x of 128 elements):
+ *   y_j  = x_j * w_j / sqrt(mean_i x_i^2 + eps)            with w = q_norm (queries) or k_norm (keys); NULL: y = x
+ *   pair i of rot_dim / 2 pairs, angle a_i = p * inv_freq[i]:
+ *   (y_u, y_v) -> magnitude * (y_u cos a_i - y_v sin a_i,  y_v cos a_i + y_u sin a_i)
+ *   with (u, v) = (i, i + rot_dim/2), or (2i, 2i + 1) if `interleaved`; elements from rot_dim on stay y.
+ * fp32 arithmetic, one rounding to bf16 at the end; the angle is reduced in fp64, so far positions lose nothing.  Scaling for
+ * long contexts is in inv_freq (any values) and magnitude. */
+typedef struct {
+  const int* positions;    /* device, n_tokens ints; any sign */
+  const float* inv_freq;   /* device, rot_dim / 2 floats (NULL if rot_dim == 0) */
+  const float* q_norm;     /* device, 128 floats, or NULL */
+  const float* k_norm;     /* device, 128 floats, or NULL */
+  float eps;               /* >= 0 */
+  float magnitude;         /* finite */
+  int rot_dim;             /* 0 .. 128, a multiple of 8 (RBS_ERR_UNSUPPORTED otherwise) */
+  int interleaved;         /* 0 or 1 */
+} rbs_rope;
+
+/*
+ * Q_out, K_out = norm and rotation of Q [batch][n_tokens][n_q_heads][128] and K [batch][n_tokens][n_kv_heads][128], whose
+ * tokens have the positions rope->positions (the same for every batch entry).  One launch.  An output may be its own input
+ * (same pointer and strides); it must not overlap an input in another way.  Head counts: any positive ones.
+ */
+RBS_API rbs_status rbs_qk_norm_rope(int batch, int n_tokens, int n_q_heads, int n_kv_heads, int head_dim, rbs_tensor Q,
+                                    rbs_tensor K, const rbs_rope* rope, rbs_tensor Q_out, rbs_tensor K_out, void* stream);
+
+/*
+ * The same for tokens of paged sequences (stride_batch of Q, K, V, Q_out, K_out is ignored; row i of them is a token):
+ * the normed and rotated key and the value of row i, as it is, go to slot slots[i] of the cache; rows whose slot is not in
+ * [0, n_pages*page_size) leave the cache alone (slots of -1 in a padded batch).  Q_out is written for every row.
+ * K_out.ptr may be NULL; otherwise it also receives the keys of every row (for a prefill call on the same tokens).
+ * Slots must differ from each other.  The caches must not overlap the other tensors.  Of the shape, n_seqs, max_pages and
+ * table_stride are not looked at.  One launch, no workspace.
+ */
+RBS_API rbs_status rbs_qk_norm_rope_paged(const rbs_paged_shape* shape, int n_tokens, rbs_tensor Q, rbs_tensor K,
+                                          rbs_tensor V, const rbs_rope* rope, const int* slots, rbs_tensor Q_out,
+                                          rbs_tensor K_out, rbs_tensor k_cache, rbs_tensor v_cache, void* stream);
+
+/*
+ * Attention of one new token of each sequence over the paged cache (the new token's own key and value stand in it already):
+ *   O_s = sum_{t < n_s} softmax_t(q_s.k_t * scale) v_t      for every query head, n_s = seq_lens[s]
+ * Q, O: row s = sequence s (stride_token, stride_head; stride_batch ignored).  bf16 inputs, fp32 accumulation and softmax, bf16
+ * output.  n_s is taken into [0, max_pages*page_size]; tokens whose page lies outside [0, n_pages) are left out.
+ * A sequence without a token gets zeros and lse = -inf.  lse (nullable): fp32 [S][Hq], natural-log-sum-exp of the scaled logits.
+ * softmax_scale == 0 means 1/sqrt(d).  The work of all sequences is cut into equal pieces on the device (no
+ * length is read on the host, so a captured graph follows them); a sequence that is cut is joined in a fixed order: a call
+ * with the same lengths gives the same bits, a sequence in another batch agrees to rounding.
+ * Workspace: rbs_paged_decode_workspace_bytes(shape) bytes, 256-byte aligned; calls that may run at the same time need
+ * one each.
+ */
+RBS_API size_t rbs_paged_decode_workspace_bytes(const rbs_paged_shape* shape);
+RBS_API rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor Q, rbs_tensor k_cache, rbs_tensor v_cache,
+                                    const int* block_table, const int* seq_lens, rbs_tensor O, float* lse,
+                                    float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Kernels that wait on hardware barriers (TMA arrival, tensor-core completion) give every wait an
  * iteration limit.  A wait that runs out records a non-zero code in a device-side status word, lets the
  * kernel drain and return, and leaves the CUDA context usable; outputs of that launch are then

@@ -22,6 +22,28 @@ rbs_status check_tensor(const rbs_tensor& t) {
   return RBS_OK;
 }
 
+static rbs_status check_pages(const rbs_paged_shape* s) {
+  if (s == nullptr || s->page_size <= 0 || s->n_pages <= 0) return RBS_ERR_INVALID_ARG;
+  if (static_cast<long long>(s->n_pages) * s->page_size > 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
+  return RBS_OK;
+}
+
+rbs_status check_paged_table(const rbs_paged_shape* s) {
+  const rbs_status st = check_pages(s);
+  if (st != RBS_OK) return st;
+  if (s->n_seqs <= 0 || s->max_pages <= 0 || s->table_stride < s->max_pages) return RBS_ERR_INVALID_ARG;
+  if (static_cast<long long>(s->max_pages) * s->page_size > 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
+  return RBS_OK;
+}
+
+rbs_status check_paged_cache(const rbs_paged_shape* s) {
+  const rbs_status st = check_pages(s);
+  if (st != RBS_OK) return st;
+  if (s->n_q_heads <= 0 || s->n_kv_heads <= 0) return RBS_ERR_INVALID_ARG;
+  if (s->head_dim != kHeadDim || s->n_q_heads % s->n_kv_heads != 0) return RBS_ERR_UNSUPPORTED;
+  return RBS_OK;
+}
+
 rbs_status check_chunk(const Dims& x, int q_start_block, int n_q_tokens) {
   if (q_start_block < 0 || n_q_tokens <= 0) return RBS_ERR_INVALID_ARG;
   const long long end = static_cast<long long>(q_start_block) * x.B + n_q_tokens;

@@ -35,6 +35,9 @@ inline Dims make_dims(const rbs_shape& s) {
 // Host-side argument checks shared by the entry points.
 rbs_status check_shape(const rbs_shape* shape);
 rbs_status check_tensor(const rbs_tensor& t);
+// Block table and pages of a paged shape; pages and heads of one.
+rbs_status check_paged_table(const rbs_paged_shape* shape);
+rbs_status check_paged_cache(const rbs_paged_shape* shape);
 struct Dims;
 // A query chunk must start on a block boundary, lie inside the sequence, and may end inside a block only at the
 // end of the sequence.

@@ -1,0 +1,393 @@
+"""The serving calls on the GPU against their fp64 oracle.
+
+Tolerances (a bf16 rounding is off by at most 2^-8 of the value).
+Norm and rotation: one rounding of the result, 2^-8 |r|; in front of it some twenty fp32 roundings of the two products a result
+is the difference of, 32 * 2^-24 of their sizes.
+Decode: the result's rounding, 2^-8 |o|; the roundings of the probabilities, 2^-8 sum(p |v|); fp32 scores of at most
+|q||k| scale ~ 40 summed over 128 products are off by about 1e-5 and their exponentials by as much, 1e-4 of sum(p |v|) covers
+both and the fp32 sums.  lse: 1e-4 for the same reason."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving_oracle as so
+from paper_2609_20971_b200 import (RbsError, alloc_step, paged_decode_workspace_bytes, rbs_device_status, rbs_paged_decode,
+                                   rbs_paged_extend, rbs_qk_norm_rope, rbs_qk_norm_rope_paged)
+
+pytestmark = pytest.mark.gpu
+STEP = 2.0 ** -8
+
+
+def _ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def _f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _randn(seed, *shape, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(torch.bfloat16)
+
+
+# ------------------------------------------------------------------------------------------------ extend
+
+
+def _extend_case(seed, seqs, page, most, old, new, n_free, n_pages, tokens, used):
+    g = np.random.default_rng(seed)
+    lens = g.integers(old[0], old[1] + 1, seqs)
+    table = g.integers(-2, n_pages + 1, (seqs, most))
+    return lens, g.integers(new[0], new[1] + 1, seqs), table, g.permutation(max(n_free, n_pages))[:n_free], used, page, n_pages, tokens
+
+
+EXTENDS = [
+    (1, 1, 16, 4, (0, 0), (1, 1), 8, 50, 1, None),              # the first token of a sequence
+    (2, 64, 64, 20, (0, 1000), (1, 1), 200, 2000, 64, 3),       # a decode step
+    (3, 7, 1, 40, (0, 9), (0, 25), 300, 400, 200, 0),           # pages of one token
+    (4, 33, 24, 9, (0, 200), (0, 60), 30, 500, 700, 11),        # pool and rows run out, tokens behind the end of the table
+    (5, 1500, 16, 6, (0, 90), (0, 40), 3000, 4000, 40000, 7),   # more sequences than threads
+    (6, 8192, 256, 3, (-5, 700), (-3, 2), 9000, 9000, 9000, 1),  # the most there may be, negative lengths
+    (7, 3, 128, 300, (0, 0), (20000, 38400), 900, 901, 100000, None),
+    (8, 5, 16, 4, (0, 60), (0, 0), 0, 10, 0, None),             # nothing new
+    (9, 5, 16, 4, (0, 60), (0, 9), 0, 10, 37, None),            # no free page at all
+]
+
+
+@pytest.mark.parametrize("seed, seqs, page, most, old, new, n_free, n_pages, tokens, used", EXTENDS)
+@pytest.mark.parametrize("wide", [0, 5])
+def test_extend_equals_the_oracle(seed, seqs, page, most, old, new, n_free, n_pages, tokens, used, wide):
+    lens, add, table, free, used, page, n_pages, tokens = _extend_case(seed, seqs, page, most, old, new, n_free, n_pages, tokens, used)
+    want = so.extend(lens, add, table, free, page, n_pages, tokens, used or 0)
+    whole = torch.full((seqs, most + wide), 77, dtype=torch.int32, device="cuda")
+    rows = whole[:, :most]
+    rows.copy_(_ints(table))
+    out = alloc_step(seqs, tokens, "cuda")
+    for t in (out.lens, out.cu, out.positions, out.slots, out.used):
+        t.fill_(-99)
+    args = (_ints(lens), _ints(add), rows, _ints(free), page, n_pages, tokens)
+    for _ in range(2):      # the same again when repeated
+        rbs_paged_extend(*args, free_used=None if used is None else _ints([used]), out=out)
+        got = [x.cpu().numpy() for x in (rows, out.lens, out.cu, out.positions, out.slots)]
+        for name, x, y in zip(("table", "lens", "cu", "positions", "slots"), got, want):
+            assert np.array_equal(x, y), name
+        assert out.used.item() == want[5]
+    assert bool((whole[:, most:] == 77).all())
+
+
+def test_extend_step_after_step_hands_out_every_page_once():
+    page, n_pages, seqs = 16, 61, 6
+    g = np.random.default_rng(3)
+    table = torch.full((seqs, 30), -1, dtype=torch.int32, device="cuda")
+    free = _ints(g.permutation(n_pages))
+    lens, used, seen = _ints([0] * seqs), _ints([0]), []
+    for _ in range(12):
+        new = g.integers(0, 19, seqs)
+        step = rbs_paged_extend(lens, _ints(new), table, free, page, n_pages, int(new.sum()) + 2, free_used=used)
+        lens, used = step.lens, step.used
+        seen += step.slots[:int(new.sum())].tolist()
+    assert min(seen) >= 0 and len(set(seen)) == len(seen) == int(lens.sum())
+
+
+# ------------------------------------------------------------------------------------------------ norm and rotation
+
+
+def _frequencies(rot, base=1e6):
+    return torch.tensor(base ** (-np.arange(0, rot, 2) / max(rot, 1)), dtype=torch.float32, device="cuda")
+
+
+def _check_turn(got, x, positions, freq, weight, **more):
+    want, size = so.norm_rope(_f64(x), positions.cpu().numpy(), [] if freq is None else _f64(freq), None if weight is None else _f64(weight), **more)
+    err = np.abs(_f64(got) - want)
+    assert (err <= STEP * np.abs(want) + 32 * 2.0 ** -24 * size).all(), float((err / (np.abs(want) + 1e-30)).max())
+
+
+@pytest.mark.parametrize("tokens, hq, hkv", [(1, 1, 1), (1, 32, 4), (3, 3, 1), (61, 40, 8), (257, 16, 16), (1003, 8, 2)])
+@pytest.mark.parametrize("rot, interleaved, norm", [(128, False, True), (128, True, True), (64, False, False), (64, True, True), (96, False, True),
+                                                    (8, True, False), (8, False, True), (0, False, True)])
+def test_norm_rope_equals_the_oracle(tokens, hq, hkv, rot, interleaved, norm):
+    x = _randn(tokens + rot, tokens, hq + 2 * hkv, 128, scale=3.0)      # slices of a fused projection
+    q, k, _ = x.split((hq, hkv, hkv), dim=1)
+    g = torch.Generator(device="cuda").manual_seed(rot)
+    pos = torch.randint(-50, 1 << 20, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    freq = None if rot == 0 else _frequencies(rot)
+    wq, wk = (torch.randn(128, generator=g, device="cuda") for _ in range(2)) if norm else (None, None)
+    before = x.clone()
+    oq, ok = rbs_qk_norm_rope(q, k, pos, freq, q_norm=wq, k_norm=wk, eps=1e-5, interleaved=interleaved, magnitude=1.25)
+    more = {"eps": 1e-5, "interleaved": interleaved, "magnitude": 1.25}
+    _check_turn(oq, q, pos, freq, wq, **more)
+    _check_turn(ok, k, pos, freq, wk, **more)
+    assert torch.equal(x, before)
+
+
+def test_norm_rope_of_a_batch_in_place_and_with_one_norm_only():
+    q, k = _randn(1, 3, 77, 6, 128), _randn(2, 3, 77, 2, 128)
+    pos, freq, w = torch.arange(77, dtype=torch.int32, device="cuda"), _frequencies(128), torch.randn(128, device="cuda")
+    q0, k0 = q.clone(), k.clone()
+    apart = rbs_qk_norm_rope(q, k, pos, freq, k_norm=w)
+    oq, ok = rbs_qk_norm_rope(q, k, pos, freq, k_norm=w, out_q=q, out_k=k)
+    assert oq is q and ok is k and torch.equal(apart[0], q) and torch.equal(apart[1], k)
+    _check_turn(q, q0, pos, freq, None)
+    _check_turn(k, k0, pos, freq, w)
+
+
+def test_angles_of_far_positions_are_exact():
+    """At position 2^31 - 1 an angle rounded to fp32 would be off by tens of radians."""
+    q = _randn(5, 6, 2, 128)
+    pos = _ints([0, 1, (1 << 24) + 1, 123456789, (1 << 31) - 1, -(1 << 31)])
+    freq = _frequencies(128, 10000.0)
+    oq, _ = rbs_qk_norm_rope(q, q, pos, freq)
+    # the oracle's own angle, rounded to fp64, is off by up to 2^31 * 2^-53 = 2.4e-7: added to the 32 roundings of 6e-8
+    want, size = so.norm_rope(_f64(q), pos.cpu().numpy(), _f64(freq))
+    assert (np.abs(_f64(oq) - want) <= STEP * np.abs(want) + 40 * 2.0 ** -24 * size).all()
+
+
+def test_norm_rope_keeps_nan_and_infinity_in_their_rows():
+    q = _randn(6, 5, 3, 128)
+    q[1, 2, 7], q[3, 0, 100] = float("nan"), float("inf")
+    pos, w = torch.arange(5, dtype=torch.int32, device="cuda"), torch.ones(128, device="cuda")
+    clean = q.clone()
+    clean[1, 2], clean[3, 0] = 1.0, 1.0
+    a, b = (rbs_qk_norm_rope(x, x, pos, _frequencies(128), q_norm=w, k_norm=w)[0] for x in (q, clean))
+    assert a[1, 2].isnan().all() and not a[3, 0].isfinite().all()
+    a[1, 2], a[3, 0] = b[1, 2], b[3, 0]
+    assert torch.equal(a, b)
+
+
+def _cache(seed, pages, page, hkv, order):
+    shape = (pages, page, hkv, 128) if order == "token" else (pages, hkv, page, 128)
+    k, v = _randn(seed, *shape), _randn(seed + 1, *shape)
+    return (k, v) if order == "token" else (k.transpose(1, 2), v.transpose(1, 2))
+
+
+@pytest.mark.parametrize("tokens, hq, hkv, page, order", [(1, 32, 4, 64, "token"), (48, 32, 4, 16, "head"), (3, 3, 1, 1, "token"), (129, 40, 8, 24, "token"),
+                                                          (700, 16, 16, 256, "head")])
+@pytest.mark.parametrize("keep_k", [False, True])
+def test_norm_rope_paged_writes_its_slots_and_nothing_else(tokens, hq, hkv, page, order, keep_k):
+    pages = tokens // page + 3
+    x = _randn(tokens, tokens, hq + 2 * hkv, 128, scale=2.0)
+    q, k, v = x.split((hq, hkv, hkv), dim=1)
+    kc, vc = _cache(7, pages, page, hkv, order)
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    slots = torch.randperm(pages * page, generator=g, device="cuda")[:tokens].int()
+    slots[1::5] = -1                      # rows of a padded batch
+    slots[2::7] = pages * page + 5        # and of a cache that is smaller than its user thinks
+    pos = torch.randint(0, 40000, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    freq, w = _frequencies(128), torch.randn(128, generator=g, device="cuda")
+    k_before, v_before = kc.clone(), vc.clone()
+    out_k = torch.empty(tokens, hkv, 128, dtype=torch.bfloat16, device="cuda") if keep_k else None
+    oq = rbs_qk_norm_rope_paged(q, k, v, pos, slots, freq, kc, vc, q_norm=w, k_norm=w, out_k=out_k)
+    want_q, want_k = rbs_qk_norm_rope(q, k, pos, freq, q_norm=w, k_norm=w)      # its own test compares it with the oracle
+    assert torch.equal(oq, want_q) and (out_k is None or torch.equal(out_k, want_k))
+    good = ((slots >= 0) & (slots < pages * page)).nonzero()[:, 0]
+    at = slots[good].long()
+    k_before[at // page, at % page], v_before[at // page, at % page] = want_k[good], v[good]
+    assert torch.equal(kc, k_before) and torch.equal(vc, v_before)
+
+
+# ------------------------------------------------------------------------------------------------ decode
+
+
+def _sequences(seed, lens, page, hkv, order="token", spare=2):
+    """A cache in which every element that belongs to no sequence is NaN, and the table: entries behind a sequence are far out of range."""
+    g = np.random.default_rng(seed)
+    need = [-(-n // page) for n in lens]
+    pages = sum(need) + spare
+    perm = g.permutation(pages)
+    table = np.full((len(lens), max(max(need), 1) + 1), 1 << 30)
+    k, v = _cache(seed, pages, page, hkv, order)
+    mine = torch.zeros(pages, page, dtype=torch.bool, device="cuda")
+    at = 0
+    for s, n in enumerate(lens):
+        table[s, :need[s]] = perm[at:at + need[s]]
+        at += need[s]
+        t = np.arange(n)
+        mine[torch.tensor(table[s, t // page], device="cuda").long(), torch.tensor(t % page, device="cuda").long()] = True
+    k[~mine], v[~mine] = float("nan"), float("nan")
+    return k, v, _ints(table), _ints(lens)
+
+
+def _check_decode(out, lse, q, k, v, table, lens, scale=None):
+    o, l, size = so.decode(_f64(q), _f64(k), _f64(v), table.cpu().numpy(), lens.cpu().numpy(), scale)
+    err = np.abs(_f64(out) - o)
+    assert (err <= STEP * np.abs(o) + (STEP + 1e-4) * size).all(), float((err - STEP * np.abs(o)).max())
+    got = _f64(lse)
+    assert np.array_equal(np.isinf(got), np.isinf(l))
+    fine = np.isfinite(l)
+    assert np.abs(got[fine] - l[fine]).max(initial=0.0) <= 1e-4
+
+
+LENS = [1, 0, 15, 16, 17, 63, 64, 65, 127, 129, 400, 0, 1000, 2, 255, 257]
+
+
+@pytest.mark.parametrize("hq, hkv", [(1, 1), (4, 2), (32, 4), (40, 8), (9, 1), (16, 1), (17, 1), (40, 1), (16, 16)])
+@pytest.mark.parametrize("page, order", [(16, "token"), (64, "head"), (1, "token"), (24, "token"), (100, "head"), (256, "token")])
+def test_decode_equals_the_oracle(hq, hkv, page, order):
+    k, v, table, lens = _sequences(hq + page, LENS, page, hkv, order)
+    q = _randn(hq, len(LENS), hq, 128, scale=1.5)
+    out, lse = rbs_paged_decode(q, k, v, table, lens, return_lse=True)
+    _check_decode(out, lse, q, k, v, table, lens)
+    again, _ = rbs_paged_decode(q, k, v, table, lens, return_lse=True)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("lens, hq, hkv, page", [
+    ([20011], 32, 4, 64), ([9000, 1], 8, 2, 128), ([1, 9000], 16, 16, 16), ([0, 5000, 0], 5, 1, 24), ([0] * 5, 8, 2, 16), ([1], 3, 1, 16),
+    ([33, 1] * 150, 4, 2, 16), ([700] * 40 + [30000], 8, 1, 256)])
+def test_decode_of_long_and_uneven_batches(lens, hq, hkv, page):
+    k, v, table, n = _sequences(len(lens), lens, page, hkv)
+    q = _randn(3, len(lens), hq, 128, scale=1.5)
+    out, lse = rbs_paged_decode(q, k, v, table, n, return_lse=True)
+    _check_decode(out, lse, q, k, v, table, n)
+
+
+def test_decode_scale_strides_and_a_narrow_table():
+    k, v, table, lens = _sequences(9, [77, 500, 3], 16, 2)
+    x = _randn(9, 3, 8 + 4, 128)
+    q = x[:, :8]                                                        # a slice of the fused projection
+    whole = torch.full((3, 10, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = whole[:, 1:9, 128:]
+    wide = torch.full((3, table.shape[1] + 3), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    for scale in (0.3, -0.05):
+        o, lse = rbs_paged_decode(q, k, v, wide[:, :table.shape[1]], lens, out=out, return_lse=True, softmax_scale=scale)
+        _check_decode(o, lse, q, k, v, table, lens, scale)
+    assert bool((whole[:, 0] == 7).all() and (whole[:, 9] == 7).all() and (whole[..., :128] == 7).all())
+    lens[1] = 1 << 30                                                   # longer than its table: as long as the table
+    cut = lens.clone()
+    cut[1] = 20 * 16
+    a, b = (rbs_paged_decode(q, k, v, table[:, :20].contiguous(), n) for n in (lens, cut))
+    assert torch.equal(a, b)
+
+
+def test_decode_leaves_out_tokens_whose_page_does_not_exist():
+    k, v, table, lens = _sequences(11, [300, 40, 64], 16, 2)
+    q = _randn(12, 3, 8, 128)
+    for s, at, page in ((0, 0, -1), (0, 7, k.shape[0]), (0, 18, -(1 << 31)), (1, 1, (1 << 31) - 1), (2, 0, -1), (2, 1, -1), (2, 2, -1), (2, 3, -1)):
+        table[s, at] = page
+    out, lse = rbs_paged_decode(q, k, v, table, lens, return_lse=True)
+    _check_decode(out, lse, q, k, v, table, lens)
+    assert bool((out[2] == 0).all() and (lse[2] == -np.inf).all())
+
+
+def test_decode_of_one_dominant_key_and_of_scores_far_apart():
+    k, v, table, lens = _sequences(13, [2000, 90], 64, 1)
+    q = _randn(14, 2, 4, 128)
+    p, o = int(table[0, 30]), 50
+    k[p, o, 0] = (q[0, 0] * 20).to(torch.bfloat16)                      # a score of some 200
+    k[int(table[1, 1]), 10:20, 0] = -(q[1, 1] * 30).to(torch.bfloat16)
+    out, lse = rbs_paged_decode(q, k, v, table, lens, return_lse=True)
+    ref, l, size = so.decode(_f64(q), _f64(k), _f64(v), table.cpu().numpy(), lens.cpu().numpy())
+    # scores of up to 350: fp32 rounding of a sum of that size, 350 * 2^-24 per addition over 8 steps of the product
+    assert (np.abs(_f64(out) - ref) <= STEP * np.abs(ref) + (STEP + 1e-3) * size).all()
+    assert np.abs(_f64(lse) - l).max() <= 1e-3
+
+
+def test_decode_passes_nan_of_a_key_on_to_the_heads_that_read_it():
+    k, v, table, lens = _sequences(15, [100, 100], 16, 2)
+    q = _randn(16, 2, 8, 128)
+    clean = rbs_paged_decode(q, k, v, table, lens)
+    k[int(table[0, 2]), 3, 1, 60] = float("nan")
+    out = rbs_paged_decode(q, k, v, table, lens)
+    assert out[0, 4:].isnan().all()
+    assert torch.equal(out[0, :4], clean[0, :4]) and torch.equal(out[1], clean[1])
+
+
+def test_offsets_beyond_32_bits():
+    """Pages 5 GB apart: byte offsets and element offsets pass 2^32 and 2^31."""
+    far = 5 * (1 << 30) // 2 // 1024 * 1024
+    room = torch.zeros(far + (1 << 20), dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.as_strided(room, (2, 16, 4, 128), (far, 512, 128, 1), at) for at in (0, 1 << 19))
+    k.copy_(_randn(1, 2, 16, 4, 128)), v.copy_(_randn(2, 2, 16, 4, 128))
+    table, lens, q = _ints([[1, 0], [1, -1]]), _ints([29, 16]), _randn(3, 2, 32, 128)
+    out, lse = rbs_paged_decode(q, k, v, table, lens, return_lse=True)
+    _check_decode(out, lse, q, k, v, table, lens)
+    x, pos, slots = _randn(4, 2, 4, 128), _ints([5, 6]), _ints([31, 3])
+    rbs_qk_norm_rope_paged(_randn(5, 2, 8, 128), x, x, pos, slots, None, k, v)
+    assert torch.equal(k[1, 15], x[0]) and torch.equal(v[0, 3], x[1])
+
+
+# ------------------------------------------------------------------------------------------------ calls together
+
+
+def test_calls_on_another_stream_and_in_a_replayed_graph():
+    """A decode step (pages and slots, norm + rotation + write, attention) captured once and replayed while lengths, inputs and
+    the cache change in place, against plain calls."""
+    page, n_pages, hq, hkv = 16, 400, 8, 2
+    start = [0, 100, 31, 700, 5]
+    S = len(start)
+    freq, w = _frequencies(64), torch.rand(128, device="cuda") + 0.5
+    free = torch.randperm(n_pages, device="cuda").int()
+
+    class State:
+        def __init__(self):
+            self.k, self.v = (torch.zeros(n_pages, page, hkv, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            self.table = torch.full((S, 60), -1, dtype=torch.int32, device="cuda")
+            self.lens, self.used, self.one = _ints([0] * S), _ints([0]), _ints([1] * S)
+            self.x = torch.empty(S, hq + 2 * hkv, 128, dtype=torch.bfloat16, device="cuda")
+            self.ws = torch.empty(paged_decode_workspace_bytes(S, hq, hkv, page, n_pages, 60), dtype=torch.uint8, device="cuda")
+            x = _randn(1, sum(start), hq + 2 * hkv, 128)
+            first = rbs_paged_extend(self.lens, _ints(start), self.table, free, page, n_pages, sum(start))
+            rbs_qk_norm_rope_paged(*x.split((hq, hkv, hkv), 1), first.positions, first.slots, freq, self.k, self.v, k_norm=w)
+            self.lens.copy_(first.lens), self.used.copy_(first.used)
+
+        def step(self):
+            st = rbs_paged_extend(self.lens, self.one, self.table, free, page, n_pages, S, free_used=self.used)
+            q = rbs_qk_norm_rope_paged(*self.x.split((hq, hkv, hkv), 1), st.positions, st.slots, freq, self.k, self.v, q_norm=w, k_norm=w)
+            out, lse = rbs_paged_decode(q, self.k, self.v, self.table, st.lens, return_lse=True, workspace=self.ws)
+            self.lens.copy_(st.lens), self.used.copy_(st.used)
+            return q, out, lse
+    a, b, side = State(), State(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.x.copy_(_randn(2, *b.x.shape))
+        b.step()
+    torch.cuda.current_stream().wait_stream(side)
+    a.x.copy_(_randn(2, *a.x.shape))
+    a.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = b.step()
+    for seed in range(3, 30):      # some sequences begin new pages on the way
+        for s in (a, b):
+            s.x.copy_(_randn(seed, *s.x.shape))
+        want = a.step()
+        graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+    assert torch.equal(a.k, b.k) and torch.equal(a.table, b.table) and torch.equal(a.lens, b.lens)
+    assert b.lens.tolist() == [n + 28 for n in start]
+    _check_decode(got[1], got[2], got[0], b.k, b.v, b.table, b.lens)
+    assert rbs_device_status() == 0
+
+
+def test_calls_refuse_what_does_not_fit_together():
+    q, cache, table, lens = _randn(1, 2, 8, 128), _randn(2, 3, 16, 2, 128), _ints([[0], [1]]), _ints([3, 4])
+    pos, freq = _ints([0, 1]), _frequencies(128)
+    k = q[:, :2].contiguous()
+    bad_decodes = [(q.float(), cache, cache, table, lens), (q, cache[..., :64], cache[..., :64], table, lens), (q, cache, cache[:2], table, lens),
+                   (q, cache, cache, table[:1], lens), (q, cache, cache, table, lens[:1]), (q, cache, cache, table, lens.long()),
+                   (q, cache, cache, table.long(), lens), (q, cache, cache, table[0], lens), (q, cache.cpu(), cache, table, lens),
+                   (q[:, :7], cache, cache, table, lens), (q[..., ::2], cache, cache, table, lens), (q[0], cache, cache, table, lens)]
+    for args in bad_decodes:
+        with pytest.raises(RbsError):
+            rbs_paged_decode(*args)
+    with pytest.raises(RbsError):
+        rbs_paged_decode(q, cache, cache, table, lens, out=torch.empty_like(q[:1]))
+    for args in [(q, k, pos[:1], freq), (q, k, pos.long(), freq), (q, k, pos, freq.double()), (q, k[:1], pos, freq), (q.half(), k, pos, freq),
+                 (q, k, pos, freq[:3]), (q, k, pos, torch.cat((freq, freq))), (q, k.cpu(), pos, freq), (q[None], k, pos, freq)]:
+        with pytest.raises(RbsError):
+            rbs_qk_norm_rope(*args)
+    with pytest.raises(RbsError):
+        rbs_qk_norm_rope(q, k, pos, freq, q_norm=torch.ones(64, device="cuda"))
+    for args in [(q, k, k[:1], pos, pos, freq, cache, cache), (q, k, k, pos, pos[:1], freq, cache, cache), (q, k, k, pos, pos, freq, cache, cache[:, :, :1]),
+                 (q, q, q, pos, pos, freq, cache, cache)]:
+        with pytest.raises(RbsError):
+            rbs_qk_norm_rope_paged(*args)
+    for args in [(lens, lens[:1], table, pos, 16, 3, 2), (lens.long(), lens, table, pos, 16, 3, 2), (lens, lens, table[:1], pos, 16, 3, 2),
+                 (lens, lens, table, pos, 0, 3, 2), (lens, lens, table, pos, 16, 3, 1 << 31)]:
+        with pytest.raises((RbsError, RuntimeError)):
+            rbs_paged_extend(*args)
+    step = alloc_step(2, 2, "cuda")
+    step.lens = lens
+    with pytest.raises(RbsError):
+        rbs_paged_extend(lens, lens, table, pos, 16, 3, 2, out=step)
