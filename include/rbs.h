@@ -366,14 +366,15 @@ RBS_API rbs_status rbs_qk_norm_rope(int batch, int n_tokens, int n_q_heads, int 
 /*
  * The same for tokens of paged sequences (stride_batch of Q, K, V, Q_out, K_out is ignored; row i of them is a token):
  * the normed and rotated key and the value of row i, as it is, go to slot slots[i] of the cache; rows whose slot is not in
- * [0, n_pages*page_size) leave the cache alone (slots of -1 in a padded batch).  Q_out is written for every row.
+ * [0, n_pages*page_size) and rows from n_slots (0 .. n_tokens) on leave the cache alone (a padded batch).  Q_out is written for
+ * every row.
  * K_out.ptr may be NULL; otherwise it also receives the keys of every row (for a prefill call on the same tokens).
  * Slots must differ from each other.  The caches must not overlap the other tensors.  Of the shape, n_seqs, max_pages and
  * table_stride are not looked at.  One launch, no workspace.
  */
 RBS_API rbs_status rbs_qk_norm_rope_paged(const rbs_paged_shape* shape, int n_tokens, rbs_tensor Q, rbs_tensor K,
-                                          rbs_tensor V, const rbs_rope* rope, const int* slots, rbs_tensor Q_out,
-                                          rbs_tensor K_out, rbs_tensor k_cache, rbs_tensor v_cache, void* stream);
+                                          rbs_tensor V, const rbs_rope* rope, const int* slots, int n_slots,
+                                          rbs_tensor Q_out, rbs_tensor K_out, rbs_tensor k_cache, rbs_tensor v_cache, void* stream);
 
 /*
  * Attention of one new token of each sequence over the paged cache (the new token's own key and value stand in it already):

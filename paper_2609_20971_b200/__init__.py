@@ -5,12 +5,12 @@ around it in a serving engine: norm and rotation of queries and keys, a paged ke
 The Python names mirror the C entry points.  Importing this package does not load the CUDA library;
 the first call does, and raises if it has not been built.
 """
-from .binding import (BlockStats, PagedStep, RbsError, alloc_stats, alloc_step, load_library, paged_decode_workspace_bytes, rbs_block_stats,
+from .binding import (BlockStats, PagedStep, RbsError, alloc_stats, alloc_step, load_library, load_native, paged_decode_workspace_bytes, rbs_block_stats,
                       rbs_block_stats_box, rbs_device_status, rbs_mask_group_union, rbs_paged_decode, rbs_paged_extend, rbs_qk_norm_rope,
                       rbs_qk_norm_rope_paged, rbs_select, rbs_select_box, rbs_select_chunk, rbs_select_static, rbs_sparse_prefill,
                       rbs_sparse_prefill_chunk, rbs_sparse_prefill_grouped, workspace_bytes)
 
-__all__ = ["BlockStats", "PagedStep", "RbsError", "alloc_stats", "alloc_step", "load_library", "paged_decode_workspace_bytes", "rbs_block_stats",
+__all__ = ["BlockStats", "PagedStep", "RbsError", "alloc_stats", "alloc_step", "load_library", "load_native", "paged_decode_workspace_bytes", "rbs_block_stats",
            "rbs_block_stats_box", "rbs_device_status", "rbs_mask_group_union", "rbs_paged_decode", "rbs_paged_extend", "rbs_qk_norm_rope",
            "rbs_qk_norm_rope_paged", "rbs_select", "rbs_select_box", "rbs_select_chunk", "rbs_select_static", "rbs_sparse_prefill",
            "rbs_sparse_prefill_chunk", "rbs_sparse_prefill_grouped", "workspace_bytes"]

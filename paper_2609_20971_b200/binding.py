@@ -7,6 +7,7 @@ streams.  There is no fallback: if the shared library is missing or a call fails
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from dataclasses import dataclass
 
@@ -108,7 +109,7 @@ def load_library() -> ctypes.CDLL:
     lib.rbs_qk_norm_rope.restype = i
     lib.rbs_qk_norm_rope.argtypes = [i, i, i, i, i, RbsTensor, RbsTensor, ctypes.POINTER(RbsRope), RbsTensor, RbsTensor, vp]
     lib.rbs_qk_norm_rope_paged.restype = i
-    lib.rbs_qk_norm_rope_paged.argtypes = [paged, i, RbsTensor, RbsTensor, RbsTensor, ctypes.POINTER(RbsRope), vp, RbsTensor,
+    lib.rbs_qk_norm_rope_paged.argtypes = [paged, i, RbsTensor, RbsTensor, RbsTensor, ctypes.POINTER(RbsRope), vp, i, RbsTensor,
                                            RbsTensor, RbsTensor, RbsTensor, vp]
     lib.rbs_paged_decode_workspace_bytes.restype = sz
     lib.rbs_paged_decode_workspace_bytes.argtypes = [paged]
@@ -472,47 +473,28 @@ def rbs_sparse_prefill_chunk(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, 
 
 
 # --------------------------------------------------------------------------------- serving: the calls around the prefill path
+# Decode steps are made of calls of a few microseconds, so these are marshalled by a native module (csrc/rbs_torch.cpp: checks
+# of the tensors, outputs, device and stream).  The current stream of the tensors' device is used, whichever device is current.
+
+NATIVE_PATH = os.path.join(_PKG, "_native.so")
+_native = None
 
 
-def _same_device(what: str, device: torch.device, tensors) -> None:
-    if device.type != "cuda":
-        raise RbsError(f"{what}: expected CUDA tensors")
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise RbsError(f"{what}: tensors on {device} and {t.device}")
-
-
-def _enqueue(what: str, device: torch.device, fn, *args) -> None:
-    """One library call on the tensors' own device (which need not be the current one) and its current stream."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream), what)
-    else:
-        with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream(device).cuda_stream), what)
-
-
-def _rows(what: str, t: torch.Tensor, dims: tuple) -> RbsTensor:
-    """A bf16 tensor [rows, heads, 128] or [batch, rows, heads, 128]; the stride of a dimension of one entry says nothing."""
-    if t.dtype != torch.bfloat16 or t.dim() != len(dims) or t.stride(-1) != 1:
-        raise RbsError(f"{what}: expected a CUDA bf16 tensor {list(dims)} with the last dimension contiguous")
-    if t.shape != dims:
-        raise RbsError(f"{what}: expected shape {list(dims)}, got {list(t.shape)}")
-    d = dims[-1]
-    stride = [st if n > 1 else d for st, n in zip(t.stride(), dims)]
-    return RbsTensor(t.data_ptr(), stride[0] if len(dims) == 4 else 0, stride[-3], stride[-2])
-
-
-def _vector(what: str, t: torch.Tensor, n: int, dtype=torch.int32):
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise RbsError(f"{what}: expected {n} contiguous {dtype} values, got {list(t.shape)} of {t.dtype}")
-    return t.data_ptr()
-
-
-def _table(what: str, t: torch.Tensor) -> tuple:
-    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] == 0 or t.shape[1] == 0 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise RbsError(f"{what}: expected an int32 block table [sequences, pages] with contiguous rows")
-    seqs, pages = t.shape
-    return seqs, pages, t.stride(0) if seqs > 1 else pages
+def load_native():
+    """The marshalling module, bound to the library; raises if it has not been built."""
+    global _native
+    if _native is None:
+        lib = load_library()
+        if not os.path.exists(NATIVE_PATH):
+            raise RbsError(f"{NATIVE_PATH} is missing: build it with `python -m paper_2609_20971_b200.build`")
+        spec = importlib.util.spec_from_file_location("paper_2609_20971_b200._native", NATIVE_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(RbsError, torch.OutOfMemoryError, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.rbs_paged_extend, lib.rbs_qk_norm_rope, lib.rbs_qk_norm_rope_paged, lib.rbs_paged_decode_workspace_bytes,
+            lib.rbs_paged_decode, lib.rbs_status_string)))
+        _native = module
+    return _native
 
 
 @dataclass
@@ -526,8 +508,7 @@ class PagedStep:
 
 
 def alloc_step(n_seqs: int, n_tokens: int, device) -> PagedStep:
-    sizes = (n_seqs, n_seqs + 1, n_tokens, n_tokens, 1)
-    return PagedStep(*torch.empty(sum(sizes), dtype=torch.int32, device=device).split(sizes))
+    return PagedStep(*(torch.empty(n, dtype=torch.int32, device=device) for n in (n_seqs, n_seqs + 1, n_tokens, n_tokens, 1)))
 
 
 def rbs_paged_extend(seq_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
@@ -537,26 +518,12 @@ def rbs_paged_extend(seq_lens: torch.Tensor, new_lens: torch.Tensor, block_table
     into `block_table` [S, max_pages] (in place); the tokens, packed sequence after sequence into n_tokens rows, get positions
     and slots (-1 in rows behind the last one, and where no page was left).  All int32 on the device.  The call does not
     advance its inputs: go on with the returned lens and used."""
-    what = "rbs_paged_extend"
-    lib = load_library()
-    dev = seq_lens.device
-    seqs, max_pages, stride = _table(what, block_table)
     if out is None:
-        out = alloc_step(seqs, n_tokens, dev)
-    _same_device(what, dev, (new_lens, block_table, free_pages, free_used, out.lens, out.cu, out.positions, out.slots, out.used))
-    shape = RbsPagedShape(seqs, 1, 1, 128, page_size, n_pages, max_pages, stride)
-    _enqueue(what, dev, lib.rbs_paged_extend, shape, _vector(what, seq_lens, seqs), _vector(what, new_lens, seqs),
-             _vector(what, free_pages, free_pages.numel()), free_pages.numel(), None if free_used is None else _vector(what, free_used, 1),
-             n_tokens, block_table.data_ptr(), _vector(what, out.lens, seqs), _vector(what, out.cu, seqs + 1),
-             _vector(what, out.positions, n_tokens), _vector(what, out.slots, n_tokens), _vector(what, out.used, 1))
+        return PagedStep(*(_native or load_native()).paged_extend(seq_lens, new_lens, block_table, free_pages, page_size, n_pages, n_tokens, free_used,
+                                                                  None, None, None, None, None))
+    (_native or load_native()).paged_extend(seq_lens, new_lens, block_table, free_pages, page_size, n_pages, n_tokens, free_used, out.lens, out.cu,
+                                            out.positions, out.slots, out.used)
     return out
-
-
-def _rope(what: str, positions, n_tokens: int, inv_freq, q_norm, k_norm, d: int, eps: float, interleaved: bool, magnitude: float) -> RbsRope:
-    pairs = 0 if inv_freq is None else inv_freq.numel()
-    return RbsRope(_vector(what, positions, n_tokens), None if pairs == 0 else _vector(what, inv_freq, pairs, torch.float32),
-                   None if q_norm is None else _vector(what, q_norm, d, torch.float32),
-                   None if k_norm is None else _vector(what, k_norm, d, torch.float32), eps, magnitude, 2 * pairs, 1 if interleaved else 0)
 
 
 def rbs_qk_norm_rope(Q: torch.Tensor, K: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor | None, *,
@@ -567,28 +534,7 @@ def rbs_qk_norm_rope(Q: torch.Tensor, K: torch.Tensor, positions: torch.Tensor, 
     2 * len(inv_freq) elements of every head, in one pass.  Q, K: [tokens, heads, 128] or [batch, tokens, heads, 128] bf16, any
     strides (slices of a fused projection); positions [tokens] int32, inv_freq fp32 (rope_frequencies; None: no rotation).
     interleaved: pairs are neighbours instead of halves apart.  out_q is Q, out_k is K: in place.  Returns (Q', K')."""
-    what = "rbs_qk_norm_rope"
-    lib = load_library()
-    if out_q is None:
-        out_q = torch.empty_like(Q)
-    if out_k is None:
-        out_k = torch.empty_like(K)
-    _same_device(what, Q.device, (K, positions, inv_freq, q_norm, k_norm, out_q, out_k))
-    if Q.dim() not in (3, 4) or K.dim() != Q.dim() or K.shape[:-2] != Q.shape[:-2]:
-        raise RbsError(f"{what}: Q and K must be [tokens, heads, 128] or [batch, tokens, heads, 128] with the same tokens")
-    T, Hq, d = Q.shape[-3:]
-    Hkv = K.shape[-2]
-    rope = _rope(what, positions, T, inv_freq, q_norm, k_norm, d, eps, interleaved, magnitude)
-    _enqueue(what, Q.device, lib.rbs_qk_norm_rope, Q.shape[0] if Q.dim() == 4 else 1, T, Hq, Hkv, d, _rows(what, Q, Q.shape),
-             _rows(what, K, (*K.shape[:-1], d)), rope, _rows(what, out_q, Q.shape), _rows(what, out_k, K.shape))
-    return out_q, out_k
-
-
-def _caches(what: str, k_cache: torch.Tensor, v_cache: torch.Tensor, d: int):
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
-        raise RbsError(f"{what}: k_cache and v_cache must be [pages, page_size, kv_heads, {d}]")
-    dims = (*k_cache.shape[:3], d)
-    return dims, _rows(what, k_cache, dims), _rows(what, v_cache, dims)
+    return (_native or load_native()).qk_norm_rope(Q, K, positions, inv_freq, q_norm, k_norm, eps, interleaved, magnitude, out_q, out_k)
 
 
 def rbs_qk_norm_rope_paged(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
@@ -597,24 +543,11 @@ def rbs_qk_norm_rope_paged(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, po
                            interleaved: bool = False, magnitude: float = 1.0, out_q: torch.Tensor | None = None,
                            out_k: torch.Tensor | None = None):
     """rbs_qk_norm_rope for tokens of paged sequences: the finished keys and the values, as they are, go to their slots of
-    k_cache, v_cache [pages, page_size, kv_heads, 128] (any strides); rows with a slot of -1 leave the cache alone.
-    Q [tokens, heads, 128], K, V [tokens, kv_heads, 128].  Returns Q'; out_k, if given, receives K' too."""
-    what = "rbs_qk_norm_rope_paged"
-    lib = load_library()
-    if Q.dim() != 3:
-        raise RbsError(f"{what}: Q must be [tokens, heads, 128]")
-    T, Hq, d = Q.shape
-    if out_q is None:
-        out_q = torch.empty_like(Q)
-    _same_device(what, Q.device, (K, V, positions, slots, inv_freq, q_norm, k_norm, k_cache, v_cache, out_q, out_k))
-    dims, kc, vc = _caches(what, k_cache, v_cache, d)
-    pages, page_size, Hkv, _ = dims
-    rope = _rope(what, positions, T, inv_freq, q_norm, k_norm, d, eps, interleaved, magnitude)
-    shape = RbsPagedShape(1, Hq, Hkv, d, page_size, pages, 1, 1)
-    _enqueue(what, Q.device, lib.rbs_qk_norm_rope_paged, shape, T, _rows(what, Q, (T, Hq, d)), _rows(what, K, (T, Hkv, d)),
-             _rows(what, V, (T, Hkv, d)), rope, _vector(what, slots, T), _rows(what, out_q, (T, Hq, d)),
-             RbsTensor(None, 0, 0, 0) if out_k is None else _rows(what, out_k, (T, Hkv, d)), kc, vc)
-    return out_q
+    k_cache, v_cache [pages, page_size, kv_heads, 128] (any strides).  Rows with a slot of -1, and rows behind the last slot where
+    there are fewer slots than tokens (a padded batch), leave the cache alone.  Q [tokens, heads, 128], K, V [tokens, kv_heads, 128].
+    Returns Q'; out_k, if given, receives K' too."""
+    return (_native or load_native()).qk_norm_rope_paged(Q, K, V, positions, inv_freq, q_norm, k_norm, eps, interleaved, magnitude, slots, k_cache,
+                                                         v_cache, out_q, out_k)
 
 
 def paged_decode_workspace_bytes(n_seqs: int, n_q_heads: int, n_kv_heads: int, page_size: int, n_pages: int, max_pages: int, d: int = 128) -> int:
@@ -630,24 +563,4 @@ def rbs_paged_decode(Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     [S, max_pages] names in k_cache, v_cache [pages, page_size, kv_heads, 128] (any strides).  Sequences of length 0 get zeros
     and lse -inf.  Returns O [S, Hq, 128] and, with return_lse, lse [S, Hq] fp32.  `workspace`: uint8, at least
     paged_decode_workspace_bytes(...); calls that may run at the same time need one each."""
-    what = "rbs_paged_decode"
-    lib = load_library()
-    if Q.dim() != 3:
-        raise RbsError(f"{what}: Q must be [sequences, heads, 128]")
-    S, Hq, d = Q.shape
-    dev = Q.device
-    dims, kc, vc = _caches(what, k_cache, v_cache, d)
-    pages, page_size, Hkv, _ = dims
-    seqs, max_pages, stride = _table(what, block_table)
-    if seqs != S:
-        raise RbsError(f"{what}: {S} rows of Q and {seqs} of the block table")
-    shape = RbsPagedShape(S, Hq, Hkv, d, page_size, pages, max_pages, stride)
-    if out is None:
-        out = torch.empty(S, Hq, d, dtype=Q.dtype, device=dev)
-    lse = torch.empty(S, Hq, dtype=torch.float32, device=dev) if return_lse else None
-    if workspace is None:
-        workspace = torch.empty(int(lib.rbs_paged_decode_workspace_bytes(shape)), dtype=torch.uint8, device=dev)
-    _same_device(what, dev, (k_cache, v_cache, block_table, seq_lens, out, workspace))
-    _enqueue(what, dev, lib.rbs_paged_decode, shape, _rows(what, Q, (S, Hq, d)), kc, vc, block_table.data_ptr(), _vector(what, seq_lens, S),
-             _rows(what, out, (S, Hq, d)), None if lse is None else lse.data_ptr(), softmax_scale, workspace.data_ptr(), workspace.numel())
-    return (out, lse) if return_lse else out
+    return (_native or load_native()).paged_decode(Q, k_cache, v_cache, block_table, seq_lens, out, return_lse, softmax_scale, workspace)

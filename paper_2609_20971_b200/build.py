@@ -12,6 +12,8 @@ LIB = os.path.join(PKG, "librbs_b200.so")
 LIB_DEBUG = os.path.join(PKG, "librbs_b200_debug.so")   # the same sources with -DRBS_DEBUG: device-side index checks
 SOURCES = ["rbs_api.cu", "rbs_tmap.cu", "rbs_stats.cu", "rbs_select.cu", "rbs_prefill.cu", "rbs_prefill_duo.cu", "rbs_union.cu", "rbs_box.cu", "rbs_varlen.cu",
            "rbs_extend.cu", "rbs_rope.cu", "rbs_decode.cu"]
+NATIVE = os.path.join(PKG, "_native.so")                # marshalling of PyTorch's tensors, see csrc/rbs_torch.cpp
+NATIVE_SOURCE = os.path.join(CSRC, "rbs_torch.cpp")
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -29,9 +31,28 @@ def needs_build(lib: str = LIB) -> bool:
     if not os.path.exists(lib):
         return True
     t = os.path.getmtime(lib)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".o")]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))]
     deps += [os.path.join(ROOT, "include", "rbs.h"), os.path.join(ROOT, "include", "rbs_selftest.h")]
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def build_native(force: bool = False) -> str:
+    """Compiles the marshalling module with the host compiler against the installed PyTorch."""
+    deps = (NATIVE_SOURCE, os.path.join(ROOT, "include", "rbs.h"))
+    if not force and os.path.exists(NATIVE) and all(os.path.getmtime(d) <= os.path.getmtime(NATIVE) for d in deps):
+        return NATIVE
+    import sysconfig
+
+    import torch
+    base = os.path.join(os.path.dirname(torch.__file__))
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    system = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
+              sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-shared",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+                    *(x for p in system for x in ("-isystem", p)), NATIVE_SOURCE, "-o", NATIVE, "-L", os.path.join(base, "lib"),
+                    "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
+    return NATIVE
 
 
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
@@ -39,6 +60,7 @@ def build_library(force: bool = False, verbose: bool = False, debug: bool = Fals
     from concurrent.futures import ThreadPoolExecutor
 
     lib = LIB_DEBUG if debug else LIB
+    build_native(force)
     if not force and not needs_build(lib):
         return lib
     suffix = ".debug.o" if debug else ".o"

@@ -354,7 +354,7 @@ template <int HT>
 __global__ void __launch_bounds__(kDecWarps * 32, 3)
 decode_kernel(const DecodeParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
-  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const uint32_t tiles = smem_u32(smem) + warp * kDecStages * 2 * kDecTileBytes;
   float* part_o = reinterpret_cast<float*>(smem + kDecOffO);
   float* part_ml = reinterpret_cast<float*>(smem + kDecOffMl);

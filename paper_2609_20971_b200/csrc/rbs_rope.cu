@@ -19,7 +19,8 @@ struct RopeParams {
   const float* q_norm;   // nullable
   const float* k_norm;   // nullable
   float eps, magnitude;
-  int rot, Hq, Hkv, N, page, n_slots;
+  int rot, Hq, Hkv, N, page;
+  int slot_rows, cache_rows;   // entries of slots; rows of the cache
   long long tokens;      // batch * N
 };
 
@@ -58,8 +59,8 @@ rope_kernel(const RopeParams p) {
     int64_t page = 0, off = 0;
     bool kept = false;
     if (PAGED) {
-      const int slot = p.slots[t];
-      kept = slot >= 0 && slot < p.n_slots;
+      const int slot = t < p.slot_rows ? p.slots[t] : -1;
+      kept = slot >= 0 && slot < p.cache_rows;
       if (kept) { page = slot / p.page; off = slot % p.page; }
     }
     const int rows = p.Hq + p.Hkv * (!PAGED ? 1 : kept ? 2 : p.Ko != nullptr ? 1 : 0);
@@ -166,13 +167,13 @@ extern "C" rbs_status rbs_qk_norm_rope(int batch, int n_tokens, int n_q_heads, i
 }
 
 extern "C" rbs_status rbs_qk_norm_rope_paged(const rbs_paged_shape* shape, int n_tokens, rbs_tensor Q, rbs_tensor K,
-                                             rbs_tensor V, const rbs_rope* rope, const int* slots, rbs_tensor Q_out,
-                                             rbs_tensor K_out, rbs_tensor k_cache, rbs_tensor v_cache, void* stream) {
+                                             rbs_tensor V, const rbs_rope* rope, const int* slots, int n_slots,
+                                             rbs_tensor Q_out, rbs_tensor K_out, rbs_tensor k_cache, rbs_tensor v_cache, void* stream) {
   using namespace rbs;
   NvtxRange range("rbs_qk_norm_rope_paged");
   rbs_status st = check_paged_cache(shape);
   if (st != RBS_OK || (st = check_rope(rope, n_tokens)) != RBS_OK) return st;
-  if (slots == nullptr) return RBS_ERR_INVALID_ARG;
+  if (n_slots < 0 || n_slots > n_tokens || (n_slots > 0 && slots == nullptr)) return RBS_ERR_INVALID_ARG;
   // rows have no batch stride here, and a tensor's stays out of the checks
   Q.stride_batch = K.stride_batch = V.stride_batch = Q_out.stride_batch = K_out.stride_batch = 0;
   if ((st = check_tensor(Q)) != RBS_OK || (st = check_tensor(K)) != RBS_OK || (st = check_tensor(V)) != RBS_OK ||
@@ -190,7 +191,7 @@ extern "C" rbs_status rbs_qk_norm_rope_paged(const rbs_paged_shape* shape, int n
   p.slots = slots;
   set_rope(p, rope);
   p.Hq = shape->n_q_heads; p.Hkv = shape->n_kv_heads; p.N = n_tokens; p.page = shape->page_size;
-  p.n_slots = shape->n_pages * shape->page_size;
+  p.slot_rows = n_slots; p.cache_rows = shape->n_pages * shape->page_size;
   p.tokens = n_tokens;
   return launch_rope(p, rope->interleaved != 0, true, static_cast<cudaStream_t>(stream));
 }

@@ -185,6 +185,19 @@ def test_norm_rope_paged_writes_its_slots_and_nothing_else(tokens, hq, hkv, page
     assert torch.equal(kc, k_before) and torch.equal(vc, v_before)
 
 
+def test_norm_rope_paged_of_a_padded_batch_with_fewer_slots_than_tokens():
+    q, k, v, kc = _randn(1, 9, 8, 128), _randn(2, 9, 2, 128), _randn(3, 9, 2, 128), torch.zeros(2, 8, 2, 128, dtype=torch.bfloat16, device="cuda")
+    vc, pos, freq = torch.zeros_like(kc), torch.arange(9, dtype=torch.int32, device="cuda"), _frequencies(128)
+    for slots in (_ints([5, 9, 2]), _ints([])):
+        kc.zero_(), vc.zero_()
+        oq = rbs_qk_norm_rope_paged(q, k, v, pos, slots, freq, kc, vc)
+        want_q, want_k = rbs_qk_norm_rope(q, k, pos, freq)
+        n, at = slots.numel(), slots.long()
+        want_kc, want_vc = torch.zeros_like(kc), torch.zeros_like(vc)
+        want_kc[at // 8, at % 8], want_vc[at // 8, at % 8] = want_k[:n], v[:n]
+        assert torch.equal(oq, want_q) and torch.equal(kc, want_kc) and torch.equal(vc, want_vc)
+
+
 # ------------------------------------------------------------------------------------------------ decode
 
 
@@ -379,7 +392,7 @@ def test_calls_refuse_what_does_not_fit_together():
             rbs_qk_norm_rope(*args)
     with pytest.raises(RbsError):
         rbs_qk_norm_rope(q, k, pos, freq, q_norm=torch.ones(64, device="cuda"))
-    for args in [(q, k, k[:1], pos, pos, freq, cache, cache), (q, k, k, pos, pos[:1], freq, cache, cache), (q, k, k, pos, pos, freq, cache, cache[:, :, :1]),
+    for args in [(q, k, k[:1], pos, pos, freq, cache, cache), (q, k, k, pos, torch.cat((pos, pos)), freq, cache, cache), (q, k, k, pos, pos, freq, cache, cache[:, :, :1]),
                  (q, q, q, pos, pos, freq, cache, cache)]:
         with pytest.raises(RbsError):
             rbs_qk_norm_rope_paged(*args)

@@ -77,7 +77,7 @@ BAD_ROWS = [_t(None), _t(P + 8), _t(st=130), _t(sh=0), _t(st=-128), _t(sh=4)]
 @pytest.mark.parametrize("change, want", BAD_TURNS)
 def test_norm_rope_refuses_rotations(lib, change, want):
     assert lib.rbs_qk_norm_rope(1, 5, 8, 2, 128, _t(), _t(), _turn(**change), _t(), _t(), None) == want
-    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, _t(), _t(), _t(), _turn(**change), P, _t(), _t(None), _t(), _t(), None) == want
+    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, _t(), _t(), _t(), _turn(**change), P, 5, _t(), _t(None), _t(), _t(), None) == want
 
 
 @pytest.mark.parametrize("which", range(4))
@@ -101,15 +101,20 @@ def test_norm_rope_paged_refuses_tensors(lib, which, bad):
     rows = [_t() for _ in range(6)]      # Q, K, V, Q', caches
     rows[which] = bad
     q, k, v, o, kc, vc = rows
-    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, q, k, v, _turn(), P, o, _t(None), kc, vc, None) == INVALID
+    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, q, k, v, _turn(), P, 5, o, _t(None), kc, vc, None) == INVALID
 
 
 def test_norm_rope_paged_refuses_shapes(lib):
     for change, want in BAD_HEADS + [(dict(page_size=0), INVALID), (dict(n_pages=0), INVALID), (dict(n_pages=1 << 20, page_size=1 << 11), UNSUPPORTED)]:
-        assert lib.rbs_qk_norm_rope_paged(_shape(**change), 5, _t(), _t(), _t(), _turn(), P, _t(), _t(None), _t(), _t(), None) == want
-    assert lib.rbs_qk_norm_rope_paged(_shape(), 0, _t(), _t(), _t(), _turn(), P, _t(), _t(None), _t(), _t(), None) == INVALID
-    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, _t(), _t(), _t(), _turn(), None, _t(), _t(None), _t(), _t(), None) == INVALID
-    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, _t(), _t(), _t(), _turn(), P, _t(), _t(st=4), _t(), _t(), None) == INVALID
+        assert lib.rbs_qk_norm_rope_paged(_shape(**change), 5, _t(), _t(), _t(), _turn(), P, 5, _t(), _t(None), _t(), _t(), None) == want
+    assert lib.rbs_qk_norm_rope_paged(_shape(), 0, _t(), _t(), _t(), _turn(), P, 5, _t(), _t(None), _t(), _t(), None) == INVALID
+    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, _t(), _t(), _t(), _turn(), None, 5, _t(), _t(None), _t(), _t(), None) == INVALID
+    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, _t(), _t(), _t(), _turn(), P, 5, _t(), _t(st=4), _t(), _t(), None) == INVALID
+
+
+@pytest.mark.parametrize("n_slots", [-1, 6])
+def test_norm_rope_paged_refuses_more_slots_than_tokens(lib, n_slots):
+    assert lib.rbs_qk_norm_rope_paged(_shape(), 5, _t(), _t(), _t(), _turn(), P, n_slots, _t(), _t(None), _t(), _t(), None) == INVALID
 
 
 def _decode(lib, shape, q=None, k=None, v=None, table=P, lens=P, o=None, scale=0.0, ws=0x100000, n=1 << 40):
@@ -131,6 +136,13 @@ def test_decode_refuses_tensors(lib, name, bad):
 @pytest.mark.parametrize("args", [dict(table=None), dict(lens=None), dict(scale=NAN), dict(scale=INF)])
 def test_decode_refuses_arguments(lib, args):
     assert _decode(lib, _shape(), **args) == INVALID
+
+
+@pytest.mark.parametrize("args", [dict(ws=None), dict(ws=0x100080), dict(n=0), dict(n=-1)])
+def test_decode_refuses_workspaces(lib, args):
+    if args.get("n") == -1:
+        args = dict(n=lib.rbs_paged_decode_workspace_bytes(_shape()) - 1)
+    assert _decode(lib, _shape(), **args) == WORKSPACE
 
 
 def test_calls_refuse_host_tensors():
