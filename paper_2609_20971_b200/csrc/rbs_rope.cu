@@ -1,6 +1,9 @@
 // rbs_qk_norm_rope and rbs_qk_norm_rope_paged: norm of each head and rotation by position in one pass over the rows of Q
 // and K (256 bytes each), in the paged form with the keys and the values going to their slots of the cache.
-// A stream: 512 bytes read and written per row against some 60 instructions of half a warp.
+// A stream: 512 bytes read and written per row against some 60 instructions of half a warp.  128K tokens of 32 + 4 heads: 367 us
+// = 6.6 TB/s, what a plain copy reaches.
+#include <type_traits>
+
 #include "rbs_common.cuh"
 
 namespace rbs {
@@ -22,177 +25,245 @@ struct RopeParams {
   int rot, Hq, Hkv, N, page;
   int slot_rows, cache_rows;   // entries of slots; rows of the cache
   long long tokens;      // batch * N
-  int halves;            // halves of warps per token: 2, 4, 8 or 16
+  int spread;            // warps per token: 1, 2, 4 or 8
 };
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeHalves = kRopeThreads / 16;   // halves of warps of a CTA
-constexpr int kRopeBatch = 4;                    // rows that half a warp has in flight
-constexpr int kRopeTokens = 8;                   // most tokens of a CTA
+constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kRopeAhead = 4;                    // pairs of rows that a warp has in flight, in shared memory
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
 
 // Half a warp per row.  Lane u (of 16) of a row holds two groups A, B of four elements:
 //   half layout, u < rot / 8: A = 4u.., B = rot/2 + 4u.., so that pair 4u + k is (A[k], B[k]);
 //   otherwise 8 neighbours: A = 8u.., B = 8u + 4..; interleaved, pairs 4u .. 4u + 3 are (A0,A1) (A2,A3) (B0,B1) (B2,B3).
 // In both layouts lane u turns pairs 4u .. 4u + 3 iff u < rot / 8: no exchange between lanes but the sum of squares, and
-// an output may be its own input.  Pair (x, y) becomes (x c0 - y s1, y c1 + x s0) * r with r = 1 / sqrt(mean + eps) and the norm's
-// weights in c and s, which stay in registers while a half walks over the heads of its token.
-template <bool INTERLEAVED>
+// an output may be its own input.  The norm's weights are in c and s, which stay in registers while a
+// half walks over the heads of its token; 1 / sqrt(mean + eps) comes last.
+// WHOLE: all of the head is turned.
+template <bool INTERLEAVED, bool WHOLE>
 struct RopeLane {
-  float c0[4], s1[4], c1[4], s0[4];
+  float2 c[4], s[4];   // element j of this lane becomes x_j c_j + x_(partner of j) s_j
   int a, b;
-  unsigned mask;     // the lanes of this half
   float eps;
-  bool turns, norm;
+  bool turns;
 
   __device__ __forceinline__ void weigh(const float2* angles, const float* weights) {
     const int u = threadIdx.x & 15;
-    norm = weights != nullptr;
-    float w[8];
+    const bool norm = weights != nullptr;
+    float w[8], cj[8], sj[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = norm ? weights[(k < 4 ? a : b - 4) + k] : 1.0f;
+    for (int j = 0; j < 8; ++j) w[j] = norm ? weights[(j < 4 ? a : b - 4) + j] : 1.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float2 cs = turns ? angles[4 * u + k] : make_float2(1.0f, 0.0f);
-      const float w0 = INTERLEAVED ? w[2 * k] : w[k], w1 = INTERLEAVED ? w[2 * k + 1] : w[4 + k];
-      c0[k] = w0 * cs.x; s1[k] = w1 * cs.y; c1[k] = w1 * cs.x; s0[k] = w0 * cs.y;
+      const float2 cs = WHOLE || turns ? angles[4 * u + k] : make_float2(1.0f, 0.0f);
+      const int f = INTERLEAVED ? 2 * k : k, g = INTERLEAVED ? 2 * k + 1 : 4 + k;
+      cj[f] = w[f] * cs.x; sj[f] = -w[g] * cs.y;
+      cj[g] = w[g] * cs.x; sj[g] = w[f] * cs.y;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      c[k] = make_float2(cj[2 * k], cj[2 * k + 1]);
+      s[k] = make_float2(sj[2 * k], sj[2 * k + 1]);
     }
   }
+  // Two neighbouring elements at a time (packed fp32 instructions).
+  template <bool NORM>
   __device__ __forceinline__ void turn(uint2& xa, uint2& xb) const {
-    const float x[8] = {bf16lo(xa.x), bf16hi(xa.x), bf16lo(xa.y), bf16hi(xa.y), bf16lo(xb.x), bf16hi(xb.x), bf16lo(xb.y), bf16hi(xb.y)};
-    float r = 1.0f;
-    if (norm) {
-      float ss = 0.f;
+    const float2 x[4] = {make_float2(bf16lo(xa.x), bf16hi(xa.x)), make_float2(bf16lo(xa.y), bf16hi(xa.y)),
+                         make_float2(bf16lo(xb.x), bf16hi(xb.x)), make_float2(bf16lo(xb.y), bf16hi(xb.y))};
+    float2 y[4];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) ss = fmaf(x[k], x[k], ss);
+    for (int k = 0; k < 4; ++k) y[k] = mul2(x[k], c[k]);
+    if (WHOLE || turns) {      // elsewhere a zero would still carry an infinite neighbour over
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(mask, ss, o);
-      r = rsqrtf(ss * (1.0f / kHeadDim) + eps);
+      for (int k = 0; k < 4; ++k) y[k] = fma2(INTERLEAVED ? make_float2(x[k].y, x[k].x) : x[k ^ 2], s[k], y[k]);
     }
-    float y[8];
+    if (NORM) {
+      float2 ss = mul2(x[0], x[0]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = INTERLEAVED ? 2 * k : k, j = INTERLEAVED ? 2 * k + 1 : 4 + k;
-      y[i] = x[i] * c0[k];
-      y[j] = x[j] * c1[k];
-      if (turns) {      // elsewhere a zero would still carry an infinite neighbour over
-        y[i] = fmaf(-x[j], s1[k], y[i]);
-        y[j] = fmaf(x[i], s0[k], y[j]);
-      }
-      if (norm) {
-        y[i] *= r;
-        y[j] *= r;
-      }
+      for (int k = 1; k < 4; ++k) ss = fma2(x[k], x[k], ss);
+      float sum = ss.x + ss.y;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const float r = rsqrtf(sum * (1.0f / kHeadDim) + eps);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = mul2(y[k], make_float2(r, r));
     }
-    xa = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-    xb = make_uint2(pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+    xa = make_uint2(pack_bf16(y[0].x, y[0].y), pack_bf16(y[1].x, y[1].y));
+    xb = make_uint2(pack_bf16(y[2].x, y[2].y), pack_bf16(y[3].x, y[3].y));
   }
 };
 
-// Up to kRopeBatch rows from head h on, every step-th.
-template <bool INTERLEAVED>
-__device__ __forceinline__ void load_rows(const RopeLane<INTERLEAVED>& lane, const __nv_bfloat16* src, int64_t stride, int h, int heads, int step,
-                                          uint2 (&xa)[kRopeBatch], uint2 (&xb)[kRopeBatch]) {
-#pragma unroll
-  for (int i = 0; i < kRopeBatch; ++i) {
-    if (h + i * step < heads) {
-      const __nv_bfloat16* row = src + (h + i * step) * stride;
-      xa[i] = *reinterpret_cast<const uint2*>(row + lane.a);
-      xb[i] = *reinterpret_cast<const uint2*>(row + lane.b);
+// The rows of one warp, two heads at a time, in order: its heads of Q, of K, of V.  kRopeAhead pairs are on their way to a ring of
+// its own in shared memory (in registers they would cost as many as the arithmetic).  All but the second head of a last pair
+// is the same for both halves, so that the warp stays together: halves that went through loops of their own took twice the
+// instructions (447 us instead of 367 for 128K tokens of 36 heads).
+struct RopeRows {
+  const __nv_bfloat16* at;       // this half's row that is fetched next, at this lane's 16 bytes
+  int64_t skip;                  // elements from it to the one behind it
+  int kind, left;                // its kind, pairs of that kind that are left
+  int head, heads, step;         // its head, of how many, heads to the one behind it
+  uint32_t ring, fill, read;     // shared memory: this half's first slot, and the byte offsets of the slots filled and read next
+
+  template <typename Open>
+  __device__ __forceinline__ void fetch(Open& open) {
+    if (left > 0) {
+      if (head < heads) cp_async16_zfill(ring + fill + (threadIdx.x & 15) * 16, at, true);
+      at += skip;
+      head += step;
+      if (--left == 0) open(*this, kind + 1);
     }
+    cp_async_commit();
+    fill = fill == (kRopeAhead - 1) * 512 ? 0 : fill + 512;
   }
+  // the next pair has arrived: the address of this half's row
+  __device__ __forceinline__ uint32_t wait() {
+    cp_async_wait<kRopeAhead - 1>();
+    __syncwarp();
+    return ring + read;
+  }
+  template <typename Open>
+  __device__ __forceinline__ void done(Open& open) {
+    __syncwarp();
+    read = read == (kRopeAhead - 1) * 512 ? 0 : read + 512;
+    fetch(open);
+  }
+};
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+  return v;
 }
 
-// The heads h, h + step, .. of one token; the first batch has been loaded.  Each row goes to one or two places.
-template <bool TURN, bool INTERLEAVED>
-__device__ __forceinline__ void walk_heads(const RopeLane<INTERLEAVED>& lane, const __nv_bfloat16* src, int64_t stride, int h, int heads, int step,
-                                           uint2 (&xa)[kRopeBatch], uint2 (&xb)[kRopeBatch], __nv_bfloat16* dst, int64_t dst_stride,
-                                           __nv_bfloat16* dst2, int64_t dst2_stride) {
-  while (h < heads) {
-#pragma unroll
-    for (int i = 0; i < kRopeBatch; ++i) {
-      const int at = h + i * step;
-      if (at < heads) {
-        if (TURN) lane.turn(xa[i], xb[i]);
-        if (dst != nullptr) {
-          *reinterpret_cast<uint2*>(dst + at * dst_stride + lane.a) = xa[i];
-          *reinterpret_cast<uint2*>(dst + at * dst_stride + lane.b) = xb[i];
-        }
-        if (dst2 != nullptr) {
-          *reinterpret_cast<uint2*>(dst2 + at * dst2_stride + lane.a) = xa[i];
-          *reinterpret_cast<uint2*>(dst2 + at * dst2_stride + lane.b) = xb[i];
-        }
-      }
-    }
-    h += kRopeBatch * step;
-    if (h < heads) load_rows(lane, src, stride, h, heads, step, xa, xb);
-  }
-}
-
-// A CTA has 16 / halves tokens, `halves` halves of warps for each.  Its threads compute the tokens' angles once, behind the
-// first rows' loads.
-template <bool INTERLEAVED, bool PAGED>
-__global__ void __launch_bounds__(kRopeThreads, 4)
+// A CTA has 8 / spread tokens, `spread` warps for each.  Its threads compute the tokens' angles once, behind the first rows'
+// loads.
+template <bool INTERLEAVED, bool WHOLE, bool PAGED>
+__global__ void __launch_bounds__(kRopeThreads, 5)
 rope_kernel(const RopeParams p) {
-  __shared__ float2 angles[kRopeTokens][kHeadDim / 2];
-  const int u = threadIdx.x & 15, half = threadIdx.x >> 4;
-  const int per_cta = kRopeHalves / p.halves, mine = half / p.halves, h0 = half - mine * p.halves;
+  __shared__ float2 angles[kRopeWarps][kHeadDim / 2];
+  __shared__ __align__(16) unsigned char rings[kRopeWarps * kRopeAhead * 512];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), u = threadIdx.x & 15, side = (threadIdx.x >> 4) & 1;
+  const int per_cta = kRopeWarps / p.spread, mine = warp / p.spread, pair0 = warp - mine * p.spread, h0 = 2 * pair0 + side;
   const long long token0 = static_cast<long long>(blockIdx.x) * per_cta, token = token0 + mine;
-  RopeLane<INTERLEAVED> lane;
-  lane.turns = u < p.rot / 8;
+  RopeLane<INTERLEAVED, WHOLE> lane;
+  lane.turns = WHOLE || u < p.rot / 8;
   lane.a = lane.turns && !INTERLEAVED ? 4 * u : 8 * u;
   lane.b = lane.turns && !INTERLEAVED ? p.rot / 2 + 4 * u : 8 * u + 4;
-  lane.mask = 0xffffu << (threadIdx.x & 16);
   lane.eps = p.eps;
   pdl_trigger();
   pdl_wait();
   const bool live = token < p.tokens;
   const int64_t l = token < p.N ? 0 : token / p.N, t = token - l * p.N;
-  const __nv_bfloat16* Q = p.Q + l * p.qsb + t * p.qst;
-  const __nv_bfloat16* K = p.K + l * p.ksb + t * p.kst;
-  const int n_q = live ? p.Hq : 0;
-  uint2 xa[kRopeBatch], xb[kRopeBatch];
-  load_rows(lane, Q, p.qsh, h0, n_q, p.halves, xa, xb);
-
-  // Angles in revolutions, as fractions of 2^64: positions are whole numbers, so whole revolutions of the frequency drop out of
-  // the product by themselves, and an angle is off by 2^-33 of a revolution at most however far the position is.
-  const int pairs = p.rot / 2;
-  for (int i = threadIdx.x; i < per_cta * (kHeadDim / 2); i += kRopeThreads) {
-    const int which = i / (kHeadDim / 2), k = i % (kHeadDim / 2);
-    if (k < pairs && token0 + which < p.tokens) {
-      double f = static_cast<double>(p.inv_freq[k]) * 0.15915494309189535;
-      f = (f - floor(f)) * 18446744073709551616.0;
-      const long long pos = p.positions[(token0 + which) % p.N];
-      const unsigned long long turn = static_cast<unsigned long long>(pos) * __double2ull_rn(f);
-      float sn, cs;
-      sincospif(static_cast<float>(static_cast<int>(turn >> 32)) * 4.656612873077393e-10f, &sn, &cs);   // 2^-31: half revolutions
-      angles[which][k] = make_float2(cs * p.magnitude, sn * p.magnitude);
-    }
-  }
-  __syncthreads();
-  if (!live) return;
-
-  lane.weigh(angles[mine], p.q_norm);
-  walk_heads<true>(lane, Q, p.qsh, h0, n_q, p.halves, xa, xb, p.Qo + l * p.qosb + t * p.qost, p.qosh, nullptr, 0);
-
   __nv_bfloat16 *kc = nullptr, *vc = nullptr;
-  if (PAGED) {
+  if (PAGED && live) {
     const int slot = t < p.slot_rows ? p.slots[t] : -1;
     if (slot >= 0 && slot < p.cache_rows) {
       const int64_t page = slot / p.page, off = slot - page * p.page;
       kc = p.Kc + page * p.kcp + off * p.kct;
       vc = p.Vc + page * p.vcp + off * p.vct;
     }
-    if (vc != nullptr) {
-      const __nv_bfloat16* V = p.V + t * p.vst;
-      load_rows(lane, V, p.vsh, h0, p.Hkv, p.halves, xa, xb);
-      walk_heads<false>(lane, V, p.vsh, h0, p.Hkv, p.halves, xa, xb, vc, p.vch, nullptr, 0);
+  }
+  // pairs of heads of this warp
+  auto pairs = [&](int heads) { return (((heads + 1) >> 1) - pair0 + p.spread - 1) / p.spread; };
+  const int n_q = live ? pairs(p.Hq) : 0;
+  const int n_k = live && (!PAGED || kc != nullptr || p.Ko != nullptr) ? pairs(p.Hkv) : 0;
+  const int n_v = PAGED && vc != nullptr ? n_k : 0;
+  const int step = 2 * p.spread;
+  auto open = [&](RopeRows& r, int kind) {      // the first row of that kind, or of the next one that there is
+    if (kind == 0 && n_q == 0) kind = 1;
+    const bool q = kind == 0, k = kind == 1;
+    if (!PAGED && !q && !k) return;
+    const int64_t stride = q ? p.qsh : k ? p.ksh : p.vsh;
+    r.at = (q ? p.Q + l * p.qsb + t * p.qst : k ? p.K + l * p.ksb + t * p.kst : p.V + t * p.vst) + h0 * stride + 8 * u;
+    r.skip = step * stride;
+    r.left = q ? n_q : k ? n_k : kind == 2 ? n_v : 0;
+    r.kind = kind;
+    r.head = h0;
+    r.heads = q ? p.Hq : p.Hkv;
+  };
+  RopeRows rows;
+  rows.step = step;
+  rows.left = 0;
+  rows.ring = smem_u32(rings) + warp * kRopeAhead * 512 + side * 256;
+  rows.fill = rows.read = 0;
+  open(rows, 0);
+#pragma unroll
+  for (int i = 0; i < kRopeAhead; ++i) rows.fetch(open);
+
+  // Angles in revolutions, as fractions of 2^64: positions are whole numbers, so whole revolutions of the frequency drop out of
+  // the product by themselves, and an angle is off by 2^-33 of a revolution at most however far the position is.
+  const int k = threadIdx.x & (kHeadDim / 2 - 1);
+  if (k < p.rot / 2) {
+    double f = static_cast<double>(p.inv_freq[k]) * 0.15915494309189535;
+    f = (f - floor(f)) * 18446744073709551616.0;
+    const unsigned long long each = __double2ull_rn(f);
+    const unsigned t0 = static_cast<unsigned>(token0 < p.N ? token0 : token0 % p.N);
+    for (int i = threadIdx.x / (kHeadDim / 2); i < per_cta && token0 + i < p.tokens; i += kRopeThreads / (kHeadDim / 2)) {
+      const unsigned at = t0 + i;
+      const long long pos = p.positions[at < static_cast<unsigned>(p.N) ? at : at % p.N];
+      float sn, cs;
+      sincospif(static_cast<float>(static_cast<int>(static_cast<unsigned long long>(pos) * each >> 32)) * 4.656612873077393e-10f, &sn,
+                &cs);      // 2^-31: in half revolutions
+      angles[i][k] = make_float2(cs * p.magnitude, sn * p.magnitude);
     }
   }
-  if (!PAGED || kc != nullptr || p.Ko != nullptr) {
-    load_rows(lane, K, p.ksh, h0, p.Hkv, p.halves, xa, xb);
+  __syncthreads();
+  if (!live) return;
+
+  const uint32_t at_a = lane.a * 2, at_b = lane.b * 2;
+  auto put = [&](__nv_bfloat16* row, const uint2& xa, const uint2& xb) {
+    *reinterpret_cast<uint2*>(row + lane.a) = xa;
+    *reinterpret_cast<uint2*>(row + lane.b) = xb;
+  };
+  auto turn_rows = [&](auto norm, int n, int heads, __nv_bfloat16* dst, int64_t skip, __nv_bfloat16* dst2, int64_t skip2) {
+    for (int i = 0, h = h0; i < n; ++i, h += step) {
+      const uint32_t from = rows.wait();
+      uint2 xa = lds64(from + at_a), xb = lds64(from + at_b);
+      rows.done(open);
+      lane.template turn<decltype(norm)::value>(xa, xb);
+      if (h < heads) {
+        if (!PAGED || dst != nullptr) put(dst, xa, xb);
+        if (PAGED && dst2 != nullptr) put(dst2, xa, xb);
+      }
+      if (!PAGED || dst != nullptr) dst += skip;
+      if (PAGED && dst2 != nullptr) dst2 += skip2;
+    }
+  };
+  if (n_q > 0) {
+    lane.weigh(angles[mine], p.q_norm);
+    __nv_bfloat16* out = p.Qo + l * p.qosb + t * p.qost + h0 * p.qosh;
+    if (p.q_norm != nullptr) turn_rows(std::true_type(), n_q, p.Hq, out, step * p.qosh, nullptr, 0);
+    else turn_rows(std::false_type(), n_q, p.Hq, out, step * p.qosh, nullptr, 0);
+  }
+  if (n_k > 0) {
     lane.weigh(angles[mine], p.k_norm);
-    walk_heads<true>(lane, K, p.ksh, h0, p.Hkv, p.halves, xa, xb, PAGED && p.Ko == nullptr ? nullptr : p.Ko + l * p.kosb + t * p.kost, p.kosh, kc,
-                     p.kch);
+    __nv_bfloat16* out = PAGED && p.Ko == nullptr ? nullptr : p.Ko + l * p.kosb + t * p.kost + h0 * p.kosh;
+    __nv_bfloat16* out2 = PAGED && kc != nullptr ? kc + h0 * p.kch : nullptr;
+    if (p.k_norm != nullptr) turn_rows(std::true_type(), n_k, p.Hkv, out, step * p.kosh, out2, step * p.kch);
+    else turn_rows(std::false_type(), n_k, p.Hkv, out, step * p.kosh, out2, step * p.kch);
+  }
+  if (PAGED) {
+    for (int i = 0, h = h0; i < n_v; ++i, h += step) {
+      const uint4 x = lds128(rows.wait() + u * 16);
+      rows.done(open);
+      if (h < p.Hkv) *reinterpret_cast<uint4*>(vc + h * p.vch + 8 * u) = x;
+    }
   }
 }
 
@@ -211,17 +282,19 @@ static void set_rope(RopeParams& p, const rbs_rope* r) {
   p.eps = r->eps; p.magnitude = r->magnitude; p.rot = r->rot_dim;
 }
 
-// A token is spread over as many halves of warps as leave all CTAs resident at a time, four per SM, and over two where that
-// does not fit.
+// A token is spread over as many warps as leave all CTAs resident at a time, four per SM; one where that does not fit.
 static rbs_status launch_rope(RopeParams p, long long tokens, bool interleaved, bool paged, cudaStream_t s) {
   const long long room = 4ll * sm_count();
-  p.halves = kRopeHalves;
-  while (p.halves > kRopeHalves / kRopeTokens && (tokens * p.halves + kRopeHalves - 1) / kRopeHalves > room) p.halves /= 2;
-  const long long per_cta = kRopeHalves / p.halves, ctas = (tokens + per_cta - 1) / per_cta;
+  p.spread = kRopeWarps;
+  while (p.spread > 1 && (tokens * p.spread + kRopeWarps - 1) / kRopeWarps > room) p.spread /= 2;
+  const long long per_cta = kRopeWarps / p.spread, ctas = (tokens + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
   p.tokens = tokens;
-  auto* kernel = paged ? (interleaved ? rope_kernel<true, true> : rope_kernel<false, true>)
-                       : (interleaved ? rope_kernel<true, false> : rope_kernel<false, false>);
+  using Kernel = void (*)(const RopeParams);
+  static const Kernel kernels[8] = {rope_kernel<false, false, false>, rope_kernel<false, false, true>, rope_kernel<false, true, false>,
+                                    rope_kernel<false, true, true>,   rope_kernel<true, false, false>, rope_kernel<true, false, true>,
+                                    rope_kernel<true, true, false>,   rope_kernel<true, true, true>};
+  const Kernel kernel = kernels[(interleaved ? 4 : 0) + (p.rot == kHeadDim ? 2 : 0) + (paged ? 1 : 0)];
   RBS_CUDA_OK(launch_pdl(kernel, static_cast<unsigned>(ctas), 1, kRopeThreads, 0, s, p));
   return RBS_OK;
 }
