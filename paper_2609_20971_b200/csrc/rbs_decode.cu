@@ -2,19 +2,26 @@
 // One pass over the keys and values with the running maximum and sum of the softmax.  The cache is read once: 512 bytes per
 // token and KV head against 4 * 128 * G operations, far below what either kind of unit can do, so HBM is the bound and all
 // else is arranged to keep loads in flight.
+//
+// The work of all sequences stands in one order -- sequence by sequence, item by item (KV head, cut of its query heads), tile by
+// tile of 16 tokens -- and is cut into equal shares, one per warp, whatever the lengths are.  A warp works alone: its own
+// ring of K and V tiles in shared memory, items that lie inside its share finished from its registers.  Only the first and
+// the last item of a share can be in pieces; pieces of one item are joined by the thread block at its end, and by a second
+// kernel where an item goes on in other thread blocks.  All joins are in the order of the tokens.
 #include "rbs_common.cuh"
 
 namespace rbs {
 
-constexpr int kDecWarps = 4;            // warps of a CTA, each with keys of its own
-constexpr int kDecKeys = 16;            // keys of a warp's tile
-constexpr int kDecTile = kDecWarps * kDecKeys;
+constexpr int kDecWarps = 4;
+constexpr int kDecCtas = 148 * 3;       // three per SM
+constexpr int kDecKeys = 16;            // tokens of a tile
 constexpr int kDecStages = 2;
-constexpr int kDecWorkers = 148 * 3;    // CTAs, three per SM
-constexpr int kDecTileBytes = kDecKeys * kHeadDim * 2;                 // K or V of a warp's tile
-constexpr int kDecRow = kHeadDim + 4;                                  // floats of a row of O on its way between warps
-constexpr int kDecOffO = kDecWarps * kDecStages * 2 * kDecTileBytes;   // two buffers [8 heads][kDecRow]
-constexpr int kDecOffMl = kDecOffO + 2 * 8 * kDecRow * 4;              // [warp][head][m, l]
+constexpr int kDecTileBytes = kDecKeys * kHeadDim * 2;                 // K or V of a tile
+constexpr int kDecRing = kDecStages * 2 * kDecTileBytes;               // of a warp
+constexpr int kDecRow = kHeadDim + 4;                                  // floats of a row of O in shared memory
+constexpr int kDecSlots = kDecCtas * (2 + kDecWarps - 1);
+constexpr int kDecItemCost = 2;         // what the end of an item costs a warp, in tiles: shares are equal with it counted
+constexpr float kDecSlack = 8.f;        // log2 units by which a score may pass the maximum in use
 
 struct DecodeParams {
   const __nv_bfloat16* Q; int64_t qst, qsh;
@@ -25,13 +32,15 @@ struct DecodeParams {
   const int* table;
   const int* lens;
   int S, Hq, Hkv, G, P, n_pages, max_pages, stride;
+  int page_tiles;  // tiles per page; 0: a tile may lie in several pages
   int cuts, gh;    // a KV head's G query heads are `cuts` items of up to gh (<= 16) heads
   int items;       // Hkv * cuts
   float scale_log2;
-  float* part_o;   // [slot][HT * 8][128] sums of parts of items
-  float2* part_ml; // [slot][HT * 8] their maxima (log2 units) and normalisers
-  int4* cut;       // [worker] the item that begins in its share and goes on: sequence (-1: none), first head | heads << 24,
-                   // slot of its first part, worker of its last part
+  // Pieces of items, [slot][HT * 8 heads]: slot 2 c: of the item that CTA c found begun, 2 c + 1: of the one that it left unfinished,
+  // 2 CTAs + 3 c + w - 1: of the item that warp w > 0 of CTA c found begun and finished
+  float* part_o;   // [..][128] sums
+  float2* part_ml; // maxima in use (log2 units) and normalisers
+  int4* found;     // [CTA] the item that its share finds begun: sequence (-1: none), first head | heads << 24, CTAs of its begin and end
 };
 
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
@@ -39,6 +48,24 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+// The value that exponentials are taken against: nothing seen yet must not give inf - inf.
+__device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (exp_base(m) + log2f(l)) * 0.6931471805599453f; }
+
+// Q^T of up to 8 * HT heads, the B operand of the eight steps over the head dimension.
+template <int HT>
+struct Queries {
+  uint32_t q[HT][16];
+  __device__ __forceinline__ void load(const __nv_bfloat16* Q, int64_t qsh, int heads) {
+    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+#pragma unroll
+    for (int n = 0; n < HT; ++n) {
+      const __nv_bfloat16* row = Q + (8 * n + g) * qsh + 2 * t;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) q[n][i] = 8 * n + g < heads ? *reinterpret_cast<const uint32_t*>(row + 8 * i) : 0u;
+    }
+  }
+};
 
 // The running softmax of up to 8 * HT heads over the keys that a warp has seen.  Keys are the M side of both products:
 //   S^T [16 keys x 8 heads] = K Q^T,   O^T [128 x 8 heads] += V^T P^T
@@ -46,18 +73,12 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
 // g + 8, of O^T elements 16 j + g and 16 j + g + 8.
 template <int HT>
 struct Softmax {
-  uint32_t q[HT][16];     // Q^T, the B operand of the eight steps over the head dimension
   float o[HT][8][4];
-  float m[HT][2], l[HT][2];   // m in units of log2; l over this lane's keys only
+  float m[HT][2], l[HT][2];   // maximum in use, log2 units; sum over this lane's keys
 
-  __device__ __forceinline__ void start(const __nv_bfloat16* Q, int64_t qsh, int heads) {
-    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  __device__ __forceinline__ void start() {
 #pragma unroll
     for (int n = 0; n < HT; ++n) {
-      const int h = 8 * n + g;
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        q[n][i] = h < heads ? *reinterpret_cast<const uint32_t*>(Q + h * qsh + 8 * i + 2 * t) : 0u;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -67,9 +88,11 @@ struct Softmax {
     }
   }
 
-  // Scores of 16 keys; `valid`: a bit per key.  p: their probabilities against the new maximum, as the B operand of P V
-  // (rounded to bf16, at most 2^-8 relative each; l sums them unrounded, so that lse does not see the rounding).
-  __device__ __forceinline__ void scores(uint32_t ktile, uint32_t valid, float scale_log2, uint32_t (&p)[HT][2]) {
+  // Scores of 16 keys; `valid`: a bit per key.  p: their probabilities against the maximum in use, as the B operand of P V
+  // (rounded to bf16, at most 2^-8 relative each; l sums them unrounded, so that lse does not see the rounding).  The maximum
+  // moves only when a score passes it by kDecSlack: probabilities of up to 2^8 round no worse, and a tile that leaves it
+  // alone has no exchange between lanes and no rescaling.
+  __device__ __forceinline__ void scores(const Queries<HT>& q, uint32_t ktile, uint32_t valid, float scale_log2, uint32_t (&p)[HT][2]) {
     const int lane = threadIdx.x & 31, g = lane >> 2;
     float c[HT][4];
 #pragma unroll
@@ -81,31 +104,45 @@ struct Softmax {
       uint32_t a[4];
       ldmatrix_x4(a[0], a[1], a[2], a[3], ktile + tile_off(lane & 15, 2 * k + (lane >> 4)));
 #pragma unroll
-      for (int n = 0; n < HT; ++n) mma_bf16_16816(c[n], a, q[n][2 * k], q[n][2 * k + 1]);
+      for (int n = 0; n < HT; ++n) mma_bf16_16816(c[n], a, q.q[n][2 * k], q.q[n][2 * k + 1]);
     }
     const bool lo = (valid >> g) & 1, hi = (valid >> (g + 8)) & 1;
+    bool move = false;
 #pragma unroll
-    for (int n = 0; n < HT; ++n) {
-      float top[2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c[n][i] = (i < 2 ? lo : hi) ? c[n][i] * scale_log2 : -INFINITY;
+    for (int n = 0; n < HT; ++n)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        top[i] = fmaxf(c[n][i], c[n][i + 2]);
+        c[n][i] = lo ? c[n][i] * scale_log2 : -INFINITY;
+        c[n][i + 2] = hi ? c[n][i + 2] * scale_log2 : -INFINITY;
+        move |= fmaxf(c[n][i], c[n][i + 2]) > m[n][i] + kDecSlack;
+      }
+    if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-        for (int s = 4; s < 32; s <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], s));
-        top[i] = fmaxf(top[i], m[n][i]);
-        const float base = top[i] == -INFINITY ? 0.f : top[i];   // nothing seen yet: no inf - inf
-        const float fade = fast_exp2(m[n][i] - base);
-        m[n][i] = top[i];
+      for (int n = 0; n < HT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float top = fmaxf(c[n][i], c[n][i + 2]);
+#pragma unroll
+          for (int s = 4; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+          top = fmaxf(top, m[n][i]);
+          const float fade = fast_exp2(m[n][i] - exp_base(top));
+          m[n][i] = top;
+          l[n][i] *= fade;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            o[n][j][i] *= fade;
+            o[n][j][i + 2] *= fade;
+          }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < HT; ++n) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float base = exp_base(m[n][i]);
         c[n][i] = fast_exp2(c[n][i] - base);
         c[n][i + 2] = fast_exp2(c[n][i + 2] - base);
-        l[n][i] = l[n][i] * fade + c[n][i] + c[n][i + 2];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          o[n][j][i] *= fade;
-          o[n][j][i + 2] *= fade;
-        }
+        l[n][i] += c[n][i] + c[n][i + 2];
       }
       p[n][0] = transpose_8x8(pack_bf16(c[n][0], c[n][1]));
       p[n][1] = transpose_8x8(pack_bf16(c[n][2], c[n][3]));
@@ -122,102 +159,83 @@ struct Softmax {
       for (int n = 0; n < HT; ++n) mma_bf16_16816(o[n][j], a, p[n][0], p[n][1]);
     }
   }
+
+  // l becomes the sum over all keys of the warp
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int n = 0; n < HT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], s);
+  }
+  // O and lse of a whole item
+  __device__ __forceinline__ void write(const DecodeParams& p, int s, int h0, int heads) const {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < HT; ++n) {
+      float inv[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        inv[i] = l[n][i] == 0.f ? 0.f : 1.0f / l[n][i];
+        const int h = 8 * n + 2 * t + i;
+        if (p.lse != nullptr && g == 0 && h < heads) p.lse[static_cast<int64_t>(s) * p.Hq + h0 + h] = lse_of(m[n][i], l[n][i]);
+      }
+      __nv_bfloat16* row = p.O + s * p.ost + (h0 + 8 * n + g) * p.osh + 2 * t;      // behind the transposition
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t x = transpose_8x8(pack_bf16(o[n][j][2 * i] * inv[0], o[n][j][2 * i + 1] * inv[1]));
+          if (8 * n + g < heads) *reinterpret_cast<uint32_t*>(row + 16 * j + 8 * i) = x;
+        }
+    }
+  }
+  // a piece of an item: rows of `stride` floats, maxima and normalisers
+  __device__ __forceinline__ void put(float* rows, int stride, float2* ml) const {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < HT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int h = 8 * n + 2 * t + i;
+        if (g == 0) ml[h] = make_float2(m[n][i], l[n][i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          rows[h * stride + 16 * j + g] = o[n][j][i];
+          rows[h * stride + 16 * j + g + 8] = o[n][j][i + 2];
+        }
+      }
+  }
 };
 
-// The sums of a CTA's warps become one: all to the largest maximum, then (0 + 2) + (1 + 3).  `whole`: the item is complete, its
-// output is written; otherwise the sum goes to the workspace.
-template <int HT>
-__device__ __forceinline__ void finish_item(const DecodeParams& p, Softmax<HT>& sm, float* part_o, float* part_ml, int s, int h0, int heads,
-                                            bool whole, int slot) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-#pragma unroll
-  for (int k = 0; k < HT; ++k) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-      for (int x = 4; x < 32; x <<= 1) sm.l[k][i] += __shfl_xor_sync(0xffffffffu, sm.l[k][i], x);
-      if (g == 0) {
-        part_ml[(warp * 8 + 2 * t + i) * 2] = sm.m[k][i];
-        part_ml[(warp * 8 + 2 * t + i) * 2 + 1] = sm.l[k][i];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) top = fmaxf(top, part_ml[(w * 8 + 2 * t + i) * 2]);
-      const float f = fast_exp2(sm.m[k][i] - (top == -INFINITY ? 0.f : top));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sm.o[k][j][i] *= f;
-        sm.o[k][j][i + 2] *= f;
-      }
-    }
-    float* mine = part_o + (warp & 1) * 8 * kDecRow;
-#pragma unroll
-    for (int round = 1; round >= 0; --round) {
-      if (warp >> 1 == round) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float* x = mine + (2 * t + (i & 1)) * kDecRow + 16 * j + g + (i >> 1) * 8;
-            *x = round == 1 ? sm.o[k][j][i] : *x + sm.o[k][j][i];
-          }
-      }
-      __syncthreads();
-    }
-    // a thread per eight elements of a head
-    const int h = threadIdx.x >> 4, c = (threadIdx.x & 15) * 8;
-    if (8 * k + h < heads) {
-      float top = -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) top = fmaxf(top, part_ml[(w * 8 + h) * 2]);
-      const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) sum += part_ml[(w * 8 + h) * 2 + 1] * fast_exp2(part_ml[(w * 8 + h) * 2] - base);
-      const float4* x = reinterpret_cast<const float4*>(part_o + h * kDecRow + c);
-      const float4* y = reinterpret_cast<const float4*>(part_o + (8 + h) * kDecRow + c);
-      float4 a = x[0], b = x[1];
-      a.x += y[0].x; a.y += y[0].y; a.z += y[0].z; a.w += y[0].w;
-      b.x += y[1].x; b.y += y[1].y; b.z += y[1].z; b.w += y[1].w;
-      if (whole) {
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        const int hq = h0 + 8 * k + h;
-        *reinterpret_cast<uint4*>(p.O + s * p.ost + hq * p.osh + c) =
-            make_uint4(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv), pack_bf16(b.x * inv, b.y * inv), pack_bf16(b.z * inv, b.w * inv));
-        if (c == 0 && p.lse != nullptr)
-          p.lse[static_cast<int64_t>(s) * p.Hq + hq] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
-      } else {
-        const int64_t row = static_cast<int64_t>(slot) * (HT * 8) + 8 * k + h;
-        float4* o = reinterpret_cast<float4*>(p.part_o + row * kHeadDim + c);
-        o[0] = a;
-        o[1] = b;
-        if (c == 0) p.part_ml[row] = make_float2(top, sum);
-      }
-    }
-    __syncthreads();
-  }
-}
-
-// A place in the order of all work: sequence by sequence, in it item by item (KV head, cut of its query heads), in it tile by
-// tile of kDecTile tokens.  A sequence has at least one tile, so that its outputs are written even if it has no token.
+// A place in the order of all work.  A sequence has at least one tile per item, so that its outputs are written even if it has
+// no token.
 struct Place {
   int s, item, tile, n, len, next_len;   // n: tiles of an item of sequence s; next_len: length of sequence s + 1
+  int hk, cut;                           // of the item
+  int page, in_page;                     // of the tile: entry of the table row, tile within the page (where pages hold whole tiles)
 };
 
 __device__ __forceinline__ int clamped_len(const DecodeParams& p, int s) {
   return s < p.S ? min(max(p.lens[s], 0), p.max_pages * p.P) : 0;
 }
-__device__ __forceinline__ int tiles_of(int len) { return len <= kDecTile ? 1 : (len - 1) / kDecTile + 1; }
+__device__ __forceinline__ int tiles_of(int len) { return len <= kDecKeys ? 1 : (len - 1) / kDecKeys + 1; }
 
 // One tile on.  True if it was the last of its item.
 __device__ __forceinline__ bool step(const DecodeParams& p, Place& at) {
+  if (++at.in_page == p.page_tiles) {
+    at.in_page = 0;
+    ++at.page;
+  }
   if (++at.tile < at.n) return false;
-  at.tile = 0;
+  at.tile = at.page = at.in_page = 0;
+  if (++at.cut == p.cuts) {
+    at.cut = 0;
+    ++at.hk;
+  }
   if (++at.item == p.items) {
-    at.item = 0;
+    at.item = at.hk = at.cut = 0;
     ++at.s;
     at.len = at.next_len;
     at.n = tiles_of(at.len);
@@ -226,48 +244,78 @@ __device__ __forceinline__ bool step(const DecodeParams& p, Place& at) {
   return true;
 }
 
-// The page-table entry of this lane's row of a warp's 16 keys (lanes 0 - 15) or values (lanes 16 - 31, the same rows).
+// The table entry of a tile, fetched a tile ahead.  WHOLE (pages hold whole tiles): one entry for the warp, and the tile's place in
+// the page; otherwise lane r or r + 16 has row r's entry and its offset in the page.
 struct Lookup {
-  int page, off, hk;
+  int page, off, count, hk;
 };
-__device__ __forceinline__ Lookup look_up(const DecodeParams& p, const Place& at, int warp) {
-  const int pos = at.tile * kDecTile + warp * kDecKeys + (threadIdx.x & 15);
-  Lookup r = {-1, 0, at.item / p.cuts};
-  if (pos < at.len) {
-    const int index = pos / p.P;
-    r.off = pos - index * p.P;
-    r.page = p.table[static_cast<int64_t>(at.s) * p.stride + index];
+template <bool WHOLE>
+__device__ __forceinline__ Lookup look_up(const DecodeParams& p, const Place& at) {
+  const int* row = p.table + static_cast<int64_t>(at.s) * p.stride;
+  Lookup r;
+  r.hk = at.hk;
+  r.page = -1;
+  r.count = min(at.len - at.tile * kDecKeys, kDecKeys);
+  if (WHOLE) {
+    r.off = at.in_page * kDecKeys;
+    if (r.count > 0) r.page = row[at.page];
+  } else {
+    const int in_tile = threadIdx.x & 15, pos = at.tile * kDecKeys + in_tile;
+    r.off = 0;
+    if (in_tile < r.count) {
+      const int index = pos / p.P;
+      r.off = pos - index * p.P;
+      r.page = row[index];
+    }
   }
   return r;
 }
 
-// Which of the 16 keys there are, a bit each, and where this lane's row starts.
-__device__ __forceinline__ uint32_t row_offset(const DecodeParams& p, const Lookup& r, int64_t& at) {
-  const bool there = r.page >= 0 && r.page < p.n_pages;
-  at = 0;
-  if (there)
-    at = (threadIdx.x & 16) ? r.page * p.vp + r.off * p.vt + r.hk * p.vh : r.page * p.kp + r.off * p.kt + r.hk * p.kh;
-  return __ballot_sync(0xffffffffu, there) & 0xffffu;
-}
+// The copies of a tile's rows; rows that are not there become zeros, so that no stale page contents reach a product.
+template <bool WHOLE>
+struct TileSource {
+  int64_t k, v;     // WHOLE: this lane's first row of keys and of values; otherwise k: lanes 0 - 15 key rows, 16 - 31 value rows
+  uint32_t valid;
 
-// Starts the copy of 16 rows, whose offsets lanes first .. first + 15 hold; rows that are not there become zeros, so that no
-// stale page contents reach a product.
-__device__ __forceinline__ void copy_rows(const __nv_bfloat16* base, int64_t at, int first, uint32_t valid, uint32_t tile) {
-  const int lane = threadIdx.x & 31, chunk = lane & 15, half = lane >> 4;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = 2 * i + half;
-    const int64_t from = __shfl_sync(0xffffffffu, at, row + first);
-    cp_async16_zfill(tile + tile_off(row, chunk), base + from + chunk * 8, (valid >> row) & 1);
+  __device__ __forceinline__ void set(const DecodeParams& p, const Lookup& r) {
+    const bool there = r.page >= 0 && r.page < p.n_pages;
+    const int lane = threadIdx.x & 31;
+    if (WHOLE) {
+      valid = there ? 0xffffu >> (kDecKeys - r.count) : 0u;
+      const int off = r.off + (lane >> 4), page = there ? r.page : 0;
+      k = page * p.kp + off * p.kt + r.hk * p.kh + (lane & 15) * 8;
+      v = page * p.vp + off * p.vt + r.hk * p.vh + (lane & 15) * 8;
+    } else {
+      k = 0;
+      if (there) k = lane >= 16 ? r.page * p.vp + r.off * p.vt + r.hk * p.vh : r.page * p.kp + r.off * p.kt + r.hk * p.kh;
+      valid = __ballot_sync(0xffffffffu, there) & 0xffffu;
+    }
   }
-  cp_async_commit();
-}
+  template <bool VALUES>
+  __device__ __forceinline__ void copy(const DecodeParams& p, uint32_t tile) const {
+    const int lane = threadIdx.x & 31, chunk = lane & 15, half = lane >> 4;
+    const __nv_bfloat16* base = VALUES ? p.V : p.K;
+    if (WHOLE) base += VALUES ? v : k;
+    const int64_t two_rows = 2 * (VALUES ? p.vt : p.kt);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = 2 * i + half;
+      const bool ok = (valid >> row) & 1;
+      if (WHOLE) {
+        cp_async16_zfill(tile + tile_off(row, chunk), base, ok);
+        base += two_rows;
+      } else {
+        const int64_t from = __shfl_sync(0xffffffffu, k, row + (VALUES ? 16 : 0));
+        cp_async16_zfill(tile + tile_off(row, chunk), base + from + chunk * 8, ok);
+      }
+    }
+  }
+};
 
-// Where tile t of all `total` tiles falls when `workers` share them in order, and where worker w's share begins.
-__device__ __forceinline__ int worker_of(long long t, long long total, int workers) {
-  return static_cast<int>(((t + 1) * workers - 1) / total);
-}
-__device__ __forceinline__ long long share_begin(int w, long long total, int workers) { return total * w / workers; }
+// Shares are cut in units of work: the tiles of an item, and behind them kDecItemCost for its end.
+// The CTA in whose share unit u of all `total` falls, and where the share of CTA c begins.
+__device__ __forceinline__ int cta_of(long long u, long long total, int ctas) { return static_cast<int>(((u + 1) * ctas - 1) / total); }
+__device__ __forceinline__ long long share_begin(int c, long long total, int ctas) { return total * c / ctas; }
 
 // Sum over the CTA of one value per thread and this thread's exclusive prefix sum.
 __device__ __forceinline__ long long scan_cta(long long v, long long* part, long long* total) {
@@ -291,20 +339,29 @@ __device__ __forceinline__ long long scan_cta(long long v, long long* part, long
   return before + x - v;
 }
 
-// Finds the total number of tiles and the place where this CTA's share of them begins.  A chunk of four lengths per thread
-// at a time; up to 512 sequences are one chunk and are read once.
-__device__ __forceinline__ void find_share(const DecodeParams& p, Place& at, long long& begin, long long& end, int& workers,
-                                           long long& all_tiles) {
+struct Share {
+  long long total;   // units of all work
+  long long begin;   // unit of this warp's first tile
+  int count;         // this warp's tiles
+  int ctas;          // that have a share
+};
+
+// Finds this warp's share and the place where it begins.  A chunk of four lengths per thread at a time; up to 512 sequences are one
+// chunk and are read once.
+__device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
   __shared__ long long part[kDecWarps];
-  __shared__ int found[2];
+  __shared__ long long within[kDecWarps + 1];      // unit within the sequence's at which warp w's share begins
+  __shared__ int2 found[kDecWarps + 1];            // that sequence, its length
   constexpr int kChunk = kDecWarps * 32 * 4;
-  int n[4];
+  const int warp = threadIdx.x >> 5;
+  int len[4], n[4];
   auto load = [&](int base) {
     int sum = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int s = base + threadIdx.x * 4 + i;
-      n[i] = s < p.S ? tiles_of(clamped_len(p, s)) : 0;
+      len[i] = clamped_len(p, s);
+      n[i] = s < p.S ? tiles_of(len[i]) + kDecItemCost : 0;
       sum += n[i];
     }
     return static_cast<long long>(sum);
@@ -316,203 +373,352 @@ __device__ __forceinline__ void find_share(const DecodeParams& p, Place& at, lon
     for (int base = 0; base < p.S; base += kChunk) sum += load(base);
     scan_cta(sum, part, &total);
   }
-  all_tiles = total * p.items;
-  workers = static_cast<int>(min(static_cast<long long>(kDecWorkers), all_tiles));
-  const int w = blockIdx.x;
-  begin = w < workers ? share_begin(w, all_tiles, workers) : all_tiles;
-  end = w < workers ? share_begin(w + 1, all_tiles, workers) : all_tiles;
-  if (begin == end) return;
-  const long long in_seqs = begin / p.items;      // tiles of one item's worth of sequences in front of the share
-  long long base_tiles = 0;
+  Share sh;
+  sh.total = total * p.items;
+  sh.ctas = static_cast<int>(min(static_cast<long long>(kDecCtas), (sh.total + kDecWarps - 1) / kDecWarps));
+  sh.begin = sh.count = 0;
+  const int c = blockIdx.x;
+  if (c >= sh.ctas) return sh;
+  const long long begin = share_begin(c, sh.total, sh.ctas), units = share_begin(c + 1, sh.total, sh.ctas) - begin;
+  if (threadIdx.x == 0) found[kDecWarps] = make_int2(p.S, 0), within[kDecWarps] = 0;      // where the share ends with all work
+  __syncthreads();
+  long long base_units = 0;
   for (int base = 0; base < p.S; base += kChunk) {
     if (p.S > kChunk) before = scan_cta(load(base), part, &total);
-    long long first = base_tiles + before;
+    long long first = (base_units + before) * p.items;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (first <= in_seqs && in_seqs < first + n[i]) {
-        found[0] = base + threadIdx.x * 4 + i;
-        found[1] = static_cast<int>(begin - first * p.items);      // the share's first tile within the sequence's
+      const long long behind = first + static_cast<long long>(n[i]) * p.items;
+#pragma unroll
+      for (int w = 0; w <= kDecWarps; ++w) {
+        const long long want = begin + units * w / kDecWarps;
+        if (first <= want && want < behind) {
+          found[w] = make_int2(base + threadIdx.x * 4 + i, len[i]);
+          within[w] = want - first;
+        }
       }
-      first += n[i];
+      first = behind;
     }
-    base_tiles += total;
-    if (in_seqs < base_tiles) break;
+    base_units += total;
+    if (begin + units < base_units * p.items) break;
   }
   __syncthreads();
-  at.s = found[0];
-  at.len = clamped_len(p, at.s);
+  // tiles in front of the place: units without those of the items' ends
+  auto place = [&](int w, Place& x) {
+    x.s = found[w].x;
+    x.len = found[w].y;
+    x.n = tiles_of(x.len);
+    const int cost = x.n + kDecItemCost;
+    x.item = static_cast<int>(within[w] / cost);
+    x.tile = static_cast<int>(within[w] - static_cast<long long>(x.item) * cost);
+    const long long unit = begin + units * w / kDecWarps, items = static_cast<long long>(x.s) * p.items + x.item;
+    return unit - max(x.tile - x.n, 0) - items * kDecItemCost;
+  };
+  Place end;
+  const long long last = place(warp + 1, end);
+  sh.count = static_cast<int>(last - place(warp, at));
+  sh.begin = begin + units * warp / kDecWarps;
   at.next_len = clamped_len(p, at.s + 1);
-  at.n = tiles_of(at.len);
-  at.item = found[1] / at.n;
-  at.tile = found[1] % at.n;
+  at.hk = at.item / p.cuts;
+  at.cut = at.item - at.hk * p.cuts;
+  at.page = at.in_page = 0;
+  if (at.tile >= at.n) {      // the end of an item: on to the next one
+    sh.begin += at.n + kDecItemCost - at.tile;
+    at.tile = at.n - 1;
+    at.in_page = -1;
+    step(p, at);
+  } else if (p.page_tiles > 0) {
+    at.page = at.tile / p.page_tiles;
+    at.in_page = at.tile - at.page * p.page_tiles;
+  }
+  return sh;
 }
 
-// One CTA per worker: an equal share of the tiles of all sequences, in order.  Items inside the share are finished here;
-// the first and the last one may reach into other shares: their sums go to the workspace (slot 2 w for the first item
-// of the share, 2 w + 1 for the last one), and the worker in whose share a cut item begins says in whole[w] which workers follow.
+// What a CTA's warps leave to its end: pieces of items, in order; piece 2 w: of the item that warp w found begun and finished (in the
+// workspace), 2 w + 1: of the one that it has left unfinished (in shared memory, where its ring was).
+struct Piece {
+  int flags, s, h0_heads;
+};
+enum { kPieceThere = 1, kPieceBegins = 2, kPieceEnds = 4 };
+
 template <int HT>
+__device__ __forceinline__ void join_pieces(const DecodeParams& p, const unsigned char* smem, const Piece* pieces) {
+  constexpr int kHeads = HT * 8;
+  const int c = blockIdx.x;
+  for (int first = 0; first < 2 * kDecWarps;) {
+    if (!(pieces[first].flags & kPieceThere)) {
+      ++first;
+      continue;
+    }
+    int last = first;      // the pieces of one item: up to one that ends it, or to the end of the share
+    for (int i = first; i < 2 * kDecWarps && !(pieces[last].flags & kPieceEnds); ++i)
+      if (pieces[i].flags & kPieceThere) last = i;
+    const bool begins = pieces[first].flags & kPieceBegins, ends = pieces[last].flags & kPieceEnds;
+    const int s = pieces[first].s, h0 = pieces[first].h0_heads & 0xffffff, heads = pieces[first].h0_heads >> 24;
+    const int slot = 2 * c + (begins ? 1 : 0);
+#pragma unroll
+    for (int n = 0; n < HT; ++n) {
+      const int h = 8 * n + (threadIdx.x >> 4), e = (threadIdx.x & 15) * 8;
+      if (h >= heads) continue;
+      auto ml_of = [&](int i) {
+        const float2* ml = i & 1 ? reinterpret_cast<const float2*>(smem + (i >> 1) * kDecRing + kHeads * kDecRow * 4)
+                                 : p.part_ml + static_cast<int64_t>(2 * kDecCtas + (kDecWarps - 1) * c + (i >> 1) - 1) * kHeads;
+        return i & 1 ? ml[h] : __ldcg(ml + h);
+      };
+      float top = -INFINITY;
+      for (int i = first; i <= last; ++i)
+        if (pieces[i].flags & kPieceThere) top = fmaxf(top, ml_of(i).x);
+      const float base = exp_base(top);
+      float acc[8] = {}, sum = 0.f;
+      for (int i = first; i <= last; ++i) {
+        if (!(pieces[i].flags & kPieceThere)) continue;
+        const float2 ml = ml_of(i);
+        const float f = fast_exp2(ml.x - base);
+        float4 a, b;
+        if (i & 1) {
+          const float4* o = reinterpret_cast<const float4*>(smem + (i >> 1) * kDecRing + (h * kDecRow + e) * 4);
+          a = o[0];
+          b = o[1];
+        } else {
+          const float4* o = reinterpret_cast<const float4*>(
+              p.part_o + (static_cast<int64_t>(2 * kDecCtas + (kDecWarps - 1) * c + (i >> 1) - 1) * kHeads + h) * kHeadDim + e);
+          a = __ldcg(o);
+          b = __ldcg(o + 1);
+        }
+        sum = fmaf(ml.y, f, sum);
+        acc[0] = fmaf(a.x, f, acc[0]); acc[1] = fmaf(a.y, f, acc[1]); acc[2] = fmaf(a.z, f, acc[2]); acc[3] = fmaf(a.w, f, acc[3]);
+        acc[4] = fmaf(b.x, f, acc[4]); acc[5] = fmaf(b.y, f, acc[5]); acc[6] = fmaf(b.z, f, acc[6]); acc[7] = fmaf(b.w, f, acc[7]);
+      }
+      if (begins && ends) {
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        *reinterpret_cast<uint4*>(p.O + s * p.ost + (h0 + h) * p.osh + e) =
+            make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv), pack_bf16(acc[4] * inv, acc[5] * inv),
+                       pack_bf16(acc[6] * inv, acc[7] * inv));
+        if (e == 0 && p.lse != nullptr) p.lse[static_cast<int64_t>(s) * p.Hq + h0 + h] = lse_of(top, sum);
+      } else {
+        const int64_t row = static_cast<int64_t>(slot) * kHeads + h;
+        float4* o = reinterpret_cast<float4*>(p.part_o + row * kHeadDim + e);
+        o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        if (e == 0) p.part_ml[row] = make_float2(top, sum);
+      }
+    }
+    first = last + 1;
+  }
+}
+
+template <int HT, bool WHOLE>
 __global__ void __launch_bounds__(kDecWarps * 32, 3)
 decode_kernel(const DecodeParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
-  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
-  const uint32_t tiles = smem_u32(smem) + warp * kDecStages * 2 * kDecTileBytes;
-  float* part_o = reinterpret_cast<float*>(smem + kDecOffO);
-  float* part_ml = reinterpret_cast<float*>(smem + kDecOffMl);
-  pdl_trigger();
+  __shared__ Piece pieces[2 * kDecWarps];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  unsigned char* ring_bytes = smem + warp * kDecRing;
+  const uint32_t ring = smem_u32(ring_bytes);
+  if (lane < 2) pieces[2 * warp + lane].flags = 0;
   pdl_wait();
   Place at;
-  long long begin, end, total;
-  int workers;
-  const int w = blockIdx.x;
-  find_share(p, at, begin, end, workers, total);
-  if (begin == end) {
-    if (threadIdx.x == 0) p.cut[w] = make_int4(-1, 0, 0, 0);
+  const Share share = find_share(p, at);
+  if (static_cast<int>(blockIdx.x) >= share.ctas) {
+    if (threadIdx.x == 0) p.found[blockIdx.x] = make_int4(-1, 0, 0, 0);
     return;
   }
-  const int count = static_cast<int>(end - begin);
-
-  // consumer's side: the item that is being summed
-  int s = at.s, item = at.item, done = 0, item_begin = at.tile == 0 ? 0 : -1;   // item_begin: in tiles of the share, -1 before it
-  bool first_item = true;
-
-  // the pipeline: tiles i + 2 on their way while tile i is worked on, the table entries of tile i + 3 as well
-  Lookup look = look_up(p, at, warp);
-  int ahead = 0;
-  auto info = [&](uint32_t valid, bool last) { return valid | (last ? 0x10000u : 0u); };
-  uint32_t queue[kDecStages];
-  int64_t from;
-  auto begin_keys = [&](uint32_t kt) {      // returns the tile's word
-    uint32_t word = 0;
-    if (ahead < count) {
-      const uint32_t valid = row_offset(p, look, from);
-      copy_rows(p.K, from, 0, valid, kt);
-      ++ahead;
-      const bool last = step(p, at);
-      if (ahead < count) look = look_up(p, at, warp);
-      word = info(valid, last);
-    } else {
-      cp_async_commit();
-    }
-    return word;
-  };
-  auto begin_values = [&](uint32_t vt, uint32_t word, bool there) {
-    if (there) copy_rows(p.V, from, 16, word & 0xffffu, vt);
-    else cp_async_commit();
-  };
-#pragma unroll
-  for (int i = 0; i < kDecStages; ++i) {
-    const bool there = ahead < count;
-    queue[i] = begin_keys(tiles + 2 * i * kDecTileBytes);
-    begin_values(tiles + (2 * i + 1) * kDecTileBytes, queue[i], there);
+  if (threadIdx.x == 0) {      // warp 0's share begins where the CTA's does
+    const long long item_begin = share.begin - at.tile;
+    p.found[blockIdx.x] = at.tile == 0 ? make_int4(-1, 0, 0, 0)
+                                       : make_int4(at.s, (at.hk * p.G + at.cut * p.gh) | min(p.gh, p.G - at.cut * p.gh) << 24,
+                                                   cta_of(item_begin, share.total, share.ctas),
+                                                   cta_of(item_begin + at.n - 1, share.total, share.ctas));
   }
+  const int count = share.count;
+  if (count > 0) {
+    // the item that is summed, and how many items this warp has begun, on the copying side and on this one
+    int s = at.s, hk = at.hk, cut = at.cut, item = at.item;
+    int item_begin = at.tile == 0 ? 0 : -1;      // tile of the share, -1: before it
+    int copied_items = 0, item_no = 0;
 
-  Softmax<HT> sm;
-  int h0 = 0, heads = 0;
-  auto open_item = [&]() {
-    const int hk = item / p.cuts, c = item - hk * p.cuts;
-    h0 = hk * p.G + c * p.gh;
-    heads = min(p.gh, p.G - c * p.gh);
-    sm.start(p.Q + s * p.qst + h0 * p.qsh, p.qsh, heads);
-  };
-  open_item();
-  for (; done < count; ++done) {
-    const uint32_t kt = tiles + 2 * (done % kDecStages) * kDecTileBytes, vt = kt + kDecTileBytes;
-    const uint32_t word = queue[0];
-    queue[0] = queue[1];
-    uint32_t pr[HT][2];
-    cp_async_wait<2 * kDecStages - 1>();
-    __syncwarp();
-    sm.scores(kt, word & 0xffffu, p.scale_log2, pr);
-    __syncwarp();
-    const bool more = ahead < count;
-    queue[1] = begin_keys(kt);
-    cp_async_wait<2 * kDecStages - 1>();
-    __syncwarp();
-    sm.values(vt, pr);
-    __syncwarp();
-    begin_values(vt, queue[1], more);
-
-    const bool last = word & 0x10000u;
-    if (!last && done + 1 < count) continue;
-    // the end of the item, or of the share
-    const bool whole = last && item_begin >= 0;
-    finish_item<HT>(p, sm, part_o, part_ml, s, h0, heads, whole, 2 * w + (first_item ? 0 : 1));
-    if (done + 1 == count) {
-      if (threadIdx.x == 0) {
-        int4 c = make_int4(-1, 0, 0, 0);
-        if (!last && item_begin >= 0)      // the item begins here and goes on; `at` stands inside it
-          c = make_int4(s, h0 | heads << 24, 2 * w + (first_item ? 0 : 1), worker_of(begin + item_begin + at.n - 1, total, workers));
-        p.cut[w] = c;
+    // tiles i + 1 and i + 2 are on their way while tile i is worked on, the table entry of tile i + 3 as well
+    Lookup look = look_up<WHOLE>(p, at);
+    TileSource<WHOLE> source;
+    int ahead = 0;
+    uint32_t queue[kDecStages];      // bits 0 - 15: the keys that there are, 16: last tile of its item
+    auto begin_keys = [&](uint32_t tile) {
+      uint32_t word = 0;
+      if (ahead < count) {
+        source.set(p, look);
+        source.template copy<false>(p, tile);
+        ++ahead;
+        const bool last = step(p, at);
+        if (ahead < count) {
+          look = look_up<WHOLE>(p, at);
+          copied_items += last;
+        }
+        word = source.valid | (last ? 0x10000u : 0u);
       }
-      break;
+      cp_async_commit();
+      return word;
+    };
+    auto begin_values = [&](uint32_t tile, bool there) {
+      if (there) source.template copy<true>(p, tile);
+      cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kDecStages; ++i) {
+      const bool there = ahead < count;
+      queue[i] = begin_keys(ring + 2 * i * kDecTileBytes);
+      begin_values(ring + (2 * i + 1) * kDecTileBytes, there);
     }
-    first_item = false;
-    item_begin = done + 1;
-    if (++item == p.items) { item = 0; ++s; }
-    open_item();
+
+    Queries<HT> q, q_next;
+    int h0, heads, next_no = 0;      // q_next: queries of item next_no of this warp, if that is ahead of item_no
+    auto heads_of = [&](int k, int c) {
+      h0 = k * p.G + c * p.gh;
+      heads = min(p.gh, p.G - c * p.gh);
+    };
+    auto fetch_next = [&]() {
+      if (HT == 1 && next_no == item_no && copied_items > item_no) {
+        int ns = s, nk = hk, nc = cut + 1;
+        if (nc == p.cuts) { nc = 0; ++nk; }
+        if (item + 1 == p.items) { nk = 0; ++ns; }
+        q_next.load(p.Q + ns * p.qst + (nk * p.G + nc * p.gh) * p.qsh, p.qsh, min(p.gh, p.G - nc * p.gh));
+        next_no = item_no + 1;
+      }
+    };
+    heads_of(hk, cut);
+    q.load(p.Q + s * p.qst + h0 * p.qsh, p.qsh, heads);
+    fetch_next();
+    Softmax<HT> sm;
+    sm.start();
+    for (int i = 0; i < count; ++i) {
+      const uint32_t kt = ring + 2 * (i % kDecStages) * kDecTileBytes, vt = kt + kDecTileBytes;
+      const uint32_t word = queue[0];
+      queue[0] = queue[1];
+      uint32_t pr[HT][2];
+      cp_async_wait<2 * kDecStages - 1>();
+      __syncwarp();
+      sm.scores(q, kt, word & 0xffffu, p.scale_log2, pr);
+      __syncwarp();
+      const bool more = ahead < count;
+      queue[1] = begin_keys(kt);
+      fetch_next();
+      cp_async_wait<2 * kDecStages - 1>();
+      __syncwarp();
+      sm.values(vt, pr);
+      __syncwarp();
+      begin_values(vt, more);
+      if (!(word & 0x10000u)) continue;
+
+      // the end of the item
+      sm.finish();
+      if (item_begin >= 0) {
+        sm.write(p, s, h0, heads);
+      } else {
+        const int64_t slot = warp == 0 ? 2 * blockIdx.x : 2 * kDecCtas + (kDecWarps - 1) * blockIdx.x + warp - 1;
+        sm.put(p.part_o + slot * (HT * 8) * kHeadDim, kHeadDim, p.part_ml + slot * (HT * 8));
+        if (warp > 0 && lane == 0) pieces[2 * warp] = {kPieceThere | kPieceEnds, s, h0 | heads << 24};
+      }
+      item_begin = i + 1;
+      ++item_no;
+      if (++cut == p.cuts) { cut = 0; ++hk; }
+      if (++item == p.items) { item = hk = 0; ++s; }
+      if (i + 1 < count) {
+        heads_of(hk, cut);
+        if (next_no == item_no) q = q_next;
+        else q.load(p.Q + s * p.qst + h0 * p.qsh, p.qsh, heads), next_no = item_no;
+        fetch_next();
+        sm.start();
+      }
+    }
+    if (item_begin < count) {      // an item is left unfinished
+      sm.finish();
+      sm.put(reinterpret_cast<float*>(ring_bytes), kDecRow, reinterpret_cast<float2*>(ring_bytes + HT * 8 * kDecRow * 4));
+      if (lane == 0) pieces[2 * warp + 1] = {kPieceThere | (item_begin >= 0 ? kPieceBegins : 0), s, h0 | heads << 24};
+    }
   }
+  pdl_trigger();      // see join_kernel
+  __syncthreads();
+  join_pieces<HT>(p, smem, pieces);
 }
 
-// Joins the parts of the item that begins in worker w's share and goes on behind it: one CTA per worker and head, a quarter of
-// the parts per warp, four elements per lane.  The order depends on the lengths alone.
+constexpr int kJoinThreads = 256;
+
+// Joins the pieces of the items that lie in several CTAs' shares.  The CTAs that found an item begun share out its 1024 * HT
+// sums: the more pieces, the narrower the strip of each, so that every CTA reads about as much as one piece holds.  Thread
+// (group, column) takes four sums of every groups-th piece, with the maximum as it goes, so that all its loads can be on
+// their way together; the groups are joined in order.  The order depends on the lengths alone.
+// It becomes resident at the end of the kernel above, and lets no later kernel do so before its own end: the kernel above fills
+// every SM exactly, and where waiting CTAs had taken places of its own its last CTAs started late (64 sequences of 64 heads:
+// 239 us instead of 218 with triggers at both kernels' begins).
 template <int HT>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const DecodeParams p) {
-  __shared__ float4 sums[3][32];
-  __shared__ float norm[3];
-  pdl_trigger();
+  __shared__ float4 sums[kJoinThreads];
+  __shared__ float2 mls[kJoinThreads];
+  constexpr int kColumns = HT * 8 * kHeadDim / 4;
   pdl_wait();
-  const int w = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int4 c = p.cut[w];
-  if (c.x < 0 || head >= c.y >> 24) return;
-  const int n = c.w - w + 1;      // part 0 in slot c.z, part i in slot 2 (w + i)
-  auto ml_of = [&](int i) { return p.part_ml[(i == 0 ? c.z : 2 * (w + i)) * (HT * 8) + head]; };
-  float top = -INFINITY;
-  for (int i = lane; i < n; i += 32) top = fmaxf(top, ml_of(i).x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const float base = top == -INFINITY ? 0.f : top;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float sum = 0.f;
+  const int4 found = p.found[blockIdx.x];
+  if (found.x < 0) return;
+  const int c0 = found.z, sharers = found.w - c0, rank = blockIdx.x - c0 - 1;
+  int width = 4;      // columns of a strip
+  while (width * sharers < kColumns) width *= 2;
+  if (rank * width >= kColumns) return;
+  const int heads = found.y >> 24, h0 = found.y & 0xffffff;
+  const int lanes = min(width, kJoinThreads), groups = kJoinThreads / lanes;
+  const int group = threadIdx.x / lanes, lane = threadIdx.x - group * lanes;
+  for (int column = rank * width + lane; column < (rank + 1) * width; column += lanes) {      // once but for strips wider than the CTA
+    const int head = column / (kHeadDim / 4);
+    float top = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (head < heads) {
 #pragma unroll 4
-  for (int i = warp; i < n; i += 4) {
-    const float2 ml = ml_of(i);
-    const float f = fast_exp2(ml.x - base);
-    const float4 o = *reinterpret_cast<const float4*>(
-        p.part_o + (static_cast<int64_t>(i == 0 ? c.z : 2 * (w + i)) * (HT * 8) + head) * kHeadDim + 4 * lane);
-    sum = fmaf(ml.y, f, sum);
-    acc.x = fmaf(o.x, f, acc.x); acc.y = fmaf(o.y, f, acc.y); acc.z = fmaf(o.z, f, acc.z); acc.w = fmaf(o.w, f, acc.w);
+      for (int i = group; i <= sharers; i += groups) {      // piece 0 in slot 2 c0 + 1, piece i in slot 2 (c0 + i)
+        const int64_t slot = i == 0 ? 2 * c0 + 1 : 2 * (c0 + i);
+        const float2 ml = p.part_ml[slot * (HT * 8) + head];
+        const float4 o = *reinterpret_cast<const float4*>(p.part_o + slot * (HT * 8 * kHeadDim) + 4 * column);
+        const float high = fmaxf(top, ml.x), base = exp_base(high);
+        const float f = fast_exp2(top - base), w = fast_exp2(ml.x - base);
+        top = high;
+        sum = sum * f + ml.y * w;
+        acc.x = acc.x * f + o.x * w; acc.y = acc.y * f + o.y * w; acc.z = acc.z * f + o.z * w; acc.w = acc.w * f + o.w * w;
+      }
+    }
+    for (int half = groups / 2; half > 0; half /= 2) {
+      __syncthreads();
+      if (group >= half && group < 2 * half) {
+        sums[threadIdx.x - half * lanes] = acc;
+        mls[threadIdx.x - half * lanes] = make_float2(top, sum);
+      }
+      __syncthreads();
+      if (group < half) {
+        const float2 ml = mls[threadIdx.x];
+        const float4 o = sums[threadIdx.x];
+        const float high = fmaxf(top, ml.x), base = exp_base(high);
+        const float f = fast_exp2(top - base), w = fast_exp2(ml.x - base);
+        top = high;
+        sum = sum * f + ml.y * w;
+        acc.x = acc.x * f + o.x * w; acc.y = acc.y * f + o.y * w; acc.z = acc.z * f + o.z * w; acc.w = acc.w * f + o.w * w;
+      }
+    }
+    if (group == 0 && head < heads) {
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      const int e = 4 * column % kHeadDim;
+      *reinterpret_cast<uint2*>(p.O + found.x * p.ost + (h0 + head) * p.osh + e) =
+          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+      if (e == 0 && p.lse != nullptr) p.lse[static_cast<int64_t>(found.x) * p.Hq + h0 + head] = lse_of(top, sum);
+    }
   }
-  if (warp > 0) {
-    sums[warp - 1][lane] = acc;
-    if (lane == 0) norm[warp - 1] = sum;
-  }
-  __syncthreads();
-  if (warp > 0) return;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const float4 o = sums[i][lane];
-    acc.x += o.x; acc.y += o.y; acc.z += o.z; acc.w += o.w;
-    sum += norm[i];
-  }
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  const int h = (c.y & 0xffffff) + head;
-  *reinterpret_cast<uint2*>(p.O + c.x * p.ost + h * p.osh + 4 * lane) =
-      make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-  if (lane == 0 && p.lse != nullptr)
-    p.lse[static_cast<int64_t>(c.x) * p.Hq + h] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
 }
 
 struct DecodeWorkspace {
-  size_t off_o, off_ml, off_cut, bytes;
+  size_t off_o, off_ml, off_found, bytes;
 };
 static DecodeWorkspace decode_workspace(int G) {
-  const size_t rows = static_cast<size_t>(2 * kDecWorkers) * (G <= 8 ? 8 : 16);
+  const size_t rows = static_cast<size_t>(kDecSlots) * (G <= 8 ? 8 : 16);
   DecodeWorkspace w;
   size_t off = 0;
   w.off_o = off; off = align_up(off + rows * kHeadDim * sizeof(float), 256);
   w.off_ml = off; off = align_up(off + rows * sizeof(float2), 256);
-  w.off_cut = off; off = align_up(off + kDecWorkers * sizeof(int4), 256);
+  w.off_found = off; off = align_up(off + kDecCtas * sizeof(int4), 256);
   w.bytes = off;
   return w;
 }
@@ -548,20 +754,24 @@ extern "C" rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor 
   p.cuts = (p.G + 15) / 16;
   p.gh = (p.G + p.cuts - 1) / p.cuts;
   p.items = p.Hkv * p.cuts;
-  if (p.Hq >= 1 << 24) return RBS_ERR_UNSUPPORTED;
+  // heads share a word with a count, a warp counts its tiles in 31 bits
+  const long long most_tiles = static_cast<long long>(p.S) * p.items * (static_cast<long long>(p.max_pages) * p.P / kDecKeys + 1);
+  if (p.Hq >= 1 << 24 || most_tiles / (kDecCtas * kDecWarps) >= 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
   const DecodeWorkspace ws = decode_workspace(p.G);
   if (workspace == nullptr || workspace_bytes < ws.bytes || reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return RBS_ERR_WORKSPACE;
   unsigned char* base = static_cast<unsigned char*>(workspace);
   p.part_o = reinterpret_cast<float*>(base + ws.off_o);
   p.part_ml = reinterpret_cast<float2*>(base + ws.off_ml);
-  p.cut = reinterpret_cast<int4*>(base + ws.off_cut);
+  p.found = reinterpret_cast<int4*>(base + ws.off_found);
   const float scale = softmax_scale == 0.f ? 1.0f / sqrtf(static_cast<float>(kHeadDim)) : softmax_scale;
   p.scale_log2 = scale * kLog2e;
-  auto* kernel = p.gh <= 8 ? decode_kernel<1> : decode_kernel<2>;
-  const size_t smem = kDecOffMl + kDecWarps * 8 * 2 * sizeof(float);
+  p.page_tiles = p.P % kDecKeys == 0 ? p.P / kDecKeys : 0;
+  auto* kernel = p.page_tiles > 0 ? (p.gh <= 8 ? decode_kernel<1, true> : decode_kernel<2, true>)
+                                  : (p.gh <= 8 ? decode_kernel<1, false> : decode_kernel<2, false>);
+  const size_t smem = static_cast<size_t>(kDecWarps) * kDecRing;
   if ((st = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem)) != RBS_OK) return st;
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  RBS_CUDA_OK(launch_pdl(kernel, kDecWorkers, 1, kDecWarps * 32, smem, cs, p));
-  RBS_CUDA_OK(launch_pdl(p.gh <= 8 ? join_kernel<1> : join_kernel<2>, kDecWorkers, p.gh, 128, 0, cs, p));
+  RBS_CUDA_OK(launch_pdl(kernel, kDecCtas, 1, kDecWarps * 32, smem, cs, p));
+  RBS_CUDA_OK(launch_pdl(p.gh <= 8 ? join_kernel<1> : join_kernel<2>, kDecCtas, 1, kJoinThreads, 0, cs, p));
   return RBS_OK;
 }
