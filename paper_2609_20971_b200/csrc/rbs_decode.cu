@@ -13,7 +13,10 @@
 namespace rbs {
 
 constexpr int kDecWarps = 4;
-constexpr int kDecCtas = 148 * 3;       // three per SM
+constexpr int kDecWave = 148 * 3;       // CTAs that are resident at a time, three per SM
+constexpr int kDecRest = 148 * 3 / 2;   // CTAs behind them, for a tenth of the work of large calls
+constexpr int kDecCtas = kDecWave + kDecRest;
+constexpr int kDecRestTiles = 32;       // where a warp's share is at least that much
 constexpr int kDecKeys = 16;            // tokens of a tile
 constexpr int kDecStages = 2;
 constexpr int kDecTileBytes = kDecKeys * kHeadDim * 2;                 // K or V of a tile
@@ -212,14 +215,13 @@ struct Softmax {
 // A place in the order of all work.  A sequence has at least one tile per item, so that its outputs are written even if it has
 // no token.
 struct Place {
-  int s, item, tile, n, len, next_len;   // n: tiles of an item of sequence s; next_len: length of sequence s + 1
+  int s, item, tile, n, len, next_len;   // n: tiles of an item of sequence s; next_len: length of sequence s + 1, as it was read
   int hk, cut;                           // of the item
   int page, in_page;                     // of the tile: entry of the table row, tile within the page (where pages hold whole tiles)
 };
 
-__device__ __forceinline__ int clamped_len(const DecodeParams& p, int s) {
-  return s < p.S ? min(max(p.lens[s], 0), p.max_pages * p.P) : 0;
-}
+__device__ __forceinline__ int read_len(const DecodeParams& p, int s) { return s < p.S ? p.lens[s] : 0; }
+__device__ __forceinline__ int clamped(const DecodeParams& p, int len) { return min(max(len, 0), p.max_pages * p.P); }
 __device__ __forceinline__ int tiles_of(int len) { return len <= kDecKeys ? 1 : (len - 1) / kDecKeys + 1; }
 
 // One tile on.  True if it was the last of its item.
@@ -237,9 +239,9 @@ __device__ __forceinline__ bool step(const DecodeParams& p, Place& at) {
   if (++at.item == p.items) {
     at.item = at.hk = at.cut = 0;
     ++at.s;
-    at.len = at.next_len;
+    at.len = clamped(p, at.next_len);
     at.n = tiles_of(at.len);
-    at.next_len = clamped_len(p, at.s + 1);
+    at.next_len = read_len(p, at.s + 1);
   }
   return true;
 }
@@ -312,24 +314,50 @@ struct TileSource {
   }
 };
 
-// Shares are cut in units of work: the tiles of an item, and behind them kDecItemCost for its end.
-// The CTA in whose share unit u of all `total` falls, and where the share of CTA c begins.
-__device__ __forceinline__ int cta_of(long long u, long long total, int ctas) { return static_cast<int>(((u + 1) * ctas - 1) / total); }
-__device__ __forceinline__ long long share_begin(int c, long long total, int ctas) { return total * c / ctas; }
+// Shares are cut in units of work: the tiles of an item, and behind them kDecItemCost for its end (in all fewer than 2^31).  The
+// first wave of CTAs gets equal shares.  CTAs do not end together, though: SMs differ in what they get of the memory
+// (128K tokens: ends between 45 and 57 us).  So large calls leave a tenth to a second wave of smaller shares, which the first
+// CTAs to end make room for: 64 sequences of 64 heads 217 -> 210 us.  In smaller ones their start costs more than that.
+struct Cuts {
+  unsigned total, first;              // units; those of the first wave
+  unsigned ctas, wave;                // CTAs with a share; those of the first wave
+  unsigned each, over, each2, over2;  // units of a share of each wave, and how many shares have one more
+
+  __device__ __forceinline__ void set(unsigned units) {
+    total = units;
+    wave = min(static_cast<unsigned>(kDecWave), (units + kDecWarps - 1) / kDecWarps);
+    const bool rest = units >= static_cast<unsigned>(kDecWave) * kDecWarps * kDecRestTiles;
+    first = rest ? units - units / 10 : units;
+    ctas = rest ? kDecCtas : wave;
+    each = first / wave;
+    over = first - each * wave;
+    each2 = (total - first) / kDecRest;
+    over2 = total - first - each2 * kDecRest;
+  }
+  __device__ __forceinline__ unsigned begin(unsigned c) const {
+    return c <= wave ? c * each + min(c, over) : first + (c - wave) * each2 + min(c - wave, over2);
+  }
+  __device__ __forceinline__ unsigned cta_of(unsigned u) const {
+    const bool in_first = u < first;
+    const unsigned x = in_first ? u : u - first, e = in_first ? each : each2, o = in_first ? over : over2;
+    const unsigned c = x < o * (e + 1) ? x / (e + 1) : o + (x - o * (e + 1)) / e;
+    return in_first ? c : wave + c;
+  }
+};
 
 // Sum over the CTA of one value per thread and this thread's exclusive prefix sum.
-__device__ __forceinline__ long long scan_cta(long long v, long long* part, long long* total) {
+__device__ __forceinline__ unsigned scan_cta(unsigned v, unsigned* part, unsigned* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long x = v;
+  unsigned x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    const unsigned y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
   __syncthreads();
   if (lane == 31) part[warp] = x;
   __syncthreads();
-  long long before = 0, all = 0;
+  unsigned before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kDecWarps; ++w) {
     before += w < warp ? part[w] : 0;
@@ -340,33 +368,33 @@ __device__ __forceinline__ long long scan_cta(long long v, long long* part, long
 }
 
 struct Share {
-  long long total;   // units of all work
-  long long begin;   // unit of this warp's first tile
+  Cuts cuts;
+  unsigned begin;    // unit of this warp's first tile
   int count;         // this warp's tiles
-  int ctas;          // that have a share
 };
 
 // Finds this warp's share and the place where it begins.  A chunk of four lengths per thread at a time; up to 512 sequences are one
 // chunk and are read once.
 __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
-  __shared__ long long part[kDecWarps];
-  __shared__ long long within[kDecWarps + 1];      // unit within the sequence's at which warp w's share begins
-  __shared__ int2 found[kDecWarps + 1];            // that sequence, its length
+  __shared__ unsigned part[kDecWarps];
+  __shared__ uint4 found[kDecWarps + 1];      // where warp w's share begins: sequence, its length, unit within it, next length
   constexpr int kChunk = kDecWarps * 32 * 4;
   const int warp = threadIdx.x >> 5;
-  int len[4], n[4];
+  int len[5];
+  unsigned n[4];
   auto load = [&](int base) {
-    int sum = 0;
+    unsigned sum = 0;
+    const int s = base + threadIdx.x * 4;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) len[i] = read_len(p, s + i);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int s = base + threadIdx.x * 4 + i;
-      len[i] = clamped_len(p, s);
-      n[i] = s < p.S ? tiles_of(len[i]) + kDecItemCost : 0;
+      n[i] = s + i < p.S ? (tiles_of(clamped(p, len[i])) + kDecItemCost) * p.items : 0;
       sum += n[i];
     }
-    return static_cast<long long>(sum);
+    return sum;
   };
-  long long total = 0, sum = 0, before = 0;
+  unsigned total = 0, sum = 0, before = 0;
   if (p.S <= kChunk) {
     before = scan_cta(load(0), part, &total);
   } else {
@@ -374,52 +402,47 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
     scan_cta(sum, part, &total);
   }
   Share sh;
-  sh.total = total * p.items;
-  sh.ctas = static_cast<int>(min(static_cast<long long>(kDecCtas), (sh.total + kDecWarps - 1) / kDecWarps));
-  sh.begin = sh.count = 0;
-  const int c = blockIdx.x;
-  if (c >= sh.ctas) return sh;
-  const long long begin = share_begin(c, sh.total, sh.ctas), units = share_begin(c + 1, sh.total, sh.ctas) - begin;
-  if (threadIdx.x == 0) found[kDecWarps] = make_int2(p.S, 0), within[kDecWarps] = 0;      // where the share ends with all work
-  __syncthreads();
-  long long base_units = 0;
+  sh.cuts.set(total);
+  sh.begin = 0;
+  sh.count = 0;
+  const unsigned c = blockIdx.x;
+  if (c >= sh.cuts.ctas) return sh;
+  const unsigned begin = sh.cuts.begin(c), units = sh.cuts.begin(c + 1) - begin;
+  unsigned seen = 0;
   for (int base = 0; base < p.S; base += kChunk) {
     if (p.S > kChunk) before = scan_cta(load(base), part, &total);
-    long long first = (base_units + before) * p.items;
+    unsigned first = seen + before;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const long long behind = first + static_cast<long long>(n[i]) * p.items;
 #pragma unroll
       for (int w = 0; w <= kDecWarps; ++w) {
-        const long long want = begin + units * w / kDecWarps;
-        if (first <= want && want < behind) {
-          found[w] = make_int2(base + threadIdx.x * 4 + i, len[i]);
-          within[w] = want - first;
-        }
+        const unsigned in = begin + units * w / kDecWarps - first;      // wraps where the sequence lies behind
+        if (in < n[i]) found[w] = make_uint4(base + threadIdx.x * 4 + i, len[i], in, len[i + 1]);
       }
-      first = behind;
+      first += n[i];
     }
-    base_units += total;
-    if (begin + units < base_units * p.items) break;
+    seen += total;
+    if (begin + units < seen) break;
   }
+  if (begin + units == sh.cuts.total && threadIdx.x == 0) found[kDecWarps] = make_uint4(p.S, 0, 0, 0);      // the end of all work
   __syncthreads();
   // tiles in front of the place: units without those of the items' ends
   auto place = [&](int w, Place& x) {
-    x.s = found[w].x;
-    x.len = found[w].y;
+    const uint4 f = found[w];
+    x.s = f.x;
+    x.len = clamped(p, f.y);
+    x.next_len = f.w;
     x.n = tiles_of(x.len);
-    const int cost = x.n + kDecItemCost;
-    x.item = static_cast<int>(within[w] / cost);
-    x.tile = static_cast<int>(within[w] - static_cast<long long>(x.item) * cost);
-    const long long unit = begin + units * w / kDecWarps, items = static_cast<long long>(x.s) * p.items + x.item;
-    return unit - max(x.tile - x.n, 0) - items * kDecItemCost;
+    const unsigned cost = x.n + kDecItemCost;
+    x.item = f.z / cost;
+    x.tile = f.z - x.item * cost;
+    return begin + units * w / kDecWarps - max(x.tile - x.n, 0) - (x.s * p.items + x.item) * kDecItemCost;
   };
   Place end;
-  const long long last = place(warp + 1, end);
-  sh.count = static_cast<int>(last - place(warp, at));
+  const unsigned last = place(warp + 1, end);
+  sh.count = last - place(warp, at);
   sh.begin = begin + units * warp / kDecWarps;
-  at.next_len = clamped_len(p, at.s + 1);
-  at.hk = at.item / p.cuts;
+  at.hk = p.cuts == 1 ? at.item : at.item / p.cuts;
   at.cut = at.item - at.hk * p.cuts;
   at.page = at.in_page = 0;
   if (at.tile >= at.n) {      // the end of an item: on to the next one
@@ -445,49 +468,58 @@ template <int HT>
 __device__ __forceinline__ void join_pieces(const DecodeParams& p, const unsigned char* smem, const Piece* pieces) {
   constexpr int kHeads = HT * 8;
   const int c = blockIdx.x;
-  for (int first = 0; first < 2 * kDecWarps;) {
-    if (!(pieces[first].flags & kPieceThere)) {
-      ++first;
-      continue;
-    }
-    int last = first;      // the pieces of one item: up to one that ends it, or to the end of the share
-    for (int i = first; i < 2 * kDecWarps && !(pieces[last].flags & kPieceEnds); ++i)
-      if (pieces[i].flags & kPieceThere) last = i;
-    const bool begins = pieces[first].flags & kPieceBegins, ends = pieces[last].flags & kPieceEnds;
+  unsigned there = 0, begun = 0, ended = 0;      // a bit per piece
+#pragma unroll
+  for (int i = 0; i < 2 * kDecWarps; ++i) {
+    const int f = pieces[i].flags;
+    there |= f & kPieceThere ? 1u << i : 0u;
+    begun |= f & kPieceBegins ? 1u << i : 0u;
+    ended |= f & kPieceEnds ? 1u << i : 0u;
+  }
+  while (there != 0) {
+    // the pieces of one item: those of shared memory up to one in the workspace that ends it, or to the end of the share
+    const int first = __ffs(there) - 1, end = ended != 0 ? __ffs(ended) - 1 : 2 * kDecWarps;
+    const unsigned mine = there & ((2u << end) - 1);
+    const bool begins = begun >> first & 1, ends = end < 2 * kDecWarps;
+    there &= ~mine;
+    ended &= ~mine;
     const int s = pieces[first].s, h0 = pieces[first].h0_heads & 0xffffff, heads = pieces[first].h0_heads >> 24;
-    const int slot = 2 * c + (begins ? 1 : 0);
 #pragma unroll
     for (int n = 0; n < HT; ++n) {
       const int h = 8 * n + (threadIdx.x >> 4), e = (threadIdx.x & 15) * 8;
       if (h >= heads) continue;
-      auto ml_of = [&](int i) {
-        const float2* ml = i & 1 ? reinterpret_cast<const float2*>(smem + (i >> 1) * kDecRing + kHeads * kDecRow * 4)
-                                 : p.part_ml + static_cast<int64_t>(2 * kDecCtas + (kDecWarps - 1) * c + (i >> 1) - 1) * kHeads;
-        return i & 1 ? ml[h] : __ldcg(ml + h);
-      };
+      float2 ml[kDecWarps + 1];
+      float4 a[kDecWarps + 1], b[kDecWarps + 1];
+#pragma unroll
+      for (int w = 0; w <= kDecWarps; ++w) {
+        ml[w] = make_float2(-INFINITY, 0.f);
+        a[w] = b[w] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (w < kDecWarps && (mine >> (2 * w + 1) & 1)) {
+          const unsigned char* from = smem + w * kDecRing;
+          ml[w] = reinterpret_cast<const float2*>(from + kHeads * kDecRow * 4)[h];
+          const float4* o = reinterpret_cast<const float4*>(from + (h * kDecRow + e) * 4);
+          a[w] = o[0];
+          b[w] = o[1];
+        }
+        if (w == kDecWarps && ends) {
+          const int64_t row = static_cast<int64_t>(2 * kDecCtas + (kDecWarps - 1) * c + (end >> 1) - 1) * kHeads + h;
+          ml[w] = __ldcg(p.part_ml + row);
+          const float4* o = reinterpret_cast<const float4*>(p.part_o + row * kHeadDim + e);
+          a[w] = __ldcg(o);
+          b[w] = __ldcg(o + 1);
+        }
+      }
       float top = -INFINITY;
-      for (int i = first; i <= last; ++i)
-        if (pieces[i].flags & kPieceThere) top = fmaxf(top, ml_of(i).x);
+#pragma unroll
+      for (int w = 0; w <= kDecWarps; ++w) top = fmaxf(top, ml[w].x);
       const float base = exp_base(top);
       float acc[8] = {}, sum = 0.f;
-      for (int i = first; i <= last; ++i) {
-        if (!(pieces[i].flags & kPieceThere)) continue;
-        const float2 ml = ml_of(i);
-        const float f = fast_exp2(ml.x - base);
-        float4 a, b;
-        if (i & 1) {
-          const float4* o = reinterpret_cast<const float4*>(smem + (i >> 1) * kDecRing + (h * kDecRow + e) * 4);
-          a = o[0];
-          b = o[1];
-        } else {
-          const float4* o = reinterpret_cast<const float4*>(
-              p.part_o + (static_cast<int64_t>(2 * kDecCtas + (kDecWarps - 1) * c + (i >> 1) - 1) * kHeads + h) * kHeadDim + e);
-          a = __ldcg(o);
-          b = __ldcg(o + 1);
-        }
-        sum = fmaf(ml.y, f, sum);
-        acc[0] = fmaf(a.x, f, acc[0]); acc[1] = fmaf(a.y, f, acc[1]); acc[2] = fmaf(a.z, f, acc[2]); acc[3] = fmaf(a.w, f, acc[3]);
-        acc[4] = fmaf(b.x, f, acc[4]); acc[5] = fmaf(b.y, f, acc[5]); acc[6] = fmaf(b.z, f, acc[6]); acc[7] = fmaf(b.w, f, acc[7]);
+#pragma unroll
+      for (int w = 0; w <= kDecWarps; ++w) {
+        const float f = fast_exp2(ml[w].x - base);
+        sum = fmaf(ml[w].y, f, sum);
+        acc[0] = fmaf(a[w].x, f, acc[0]); acc[1] = fmaf(a[w].y, f, acc[1]); acc[2] = fmaf(a[w].z, f, acc[2]); acc[3] = fmaf(a[w].w, f, acc[3]);
+        acc[4] = fmaf(b[w].x, f, acc[4]); acc[5] = fmaf(b[w].y, f, acc[5]); acc[6] = fmaf(b[w].z, f, acc[6]); acc[7] = fmaf(b[w].w, f, acc[7]);
       }
       if (begins && ends) {
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
@@ -496,14 +528,13 @@ __device__ __forceinline__ void join_pieces(const DecodeParams& p, const unsigne
                        pack_bf16(acc[6] * inv, acc[7] * inv));
         if (e == 0 && p.lse != nullptr) p.lse[static_cast<int64_t>(s) * p.Hq + h0 + h] = lse_of(top, sum);
       } else {
-        const int64_t row = static_cast<int64_t>(slot) * kHeads + h;
+        const int64_t row = static_cast<int64_t>(2 * c + (begins ? 1 : 0)) * kHeads + h;
         float4* o = reinterpret_cast<float4*>(p.part_o + row * kHeadDim + e);
         o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
         o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
         if (e == 0) p.part_ml[row] = make_float2(top, sum);
       }
     }
-    first = last + 1;
   }
 }
 
@@ -519,17 +550,18 @@ decode_kernel(const DecodeParams p) {
   pdl_wait();
   Place at;
   const Share share = find_share(p, at);
-  if (static_cast<int>(blockIdx.x) >= share.ctas) {
+  if (blockIdx.x >= share.cuts.ctas) {
     if (threadIdx.x == 0) p.found[blockIdx.x] = make_int4(-1, 0, 0, 0);
     return;
   }
-  if (threadIdx.x == 0) {      // warp 0's share begins where the CTA's does
-    const long long item_begin = share.begin - at.tile;
-    p.found[blockIdx.x] = at.tile == 0 ? make_int4(-1, 0, 0, 0)
-                                       : make_int4(at.s, (at.hk * p.G + at.cut * p.gh) | min(p.gh, p.G - at.cut * p.gh) << 24,
-                                                   cta_of(item_begin, share.total, share.ctas),
-                                                   cta_of(item_begin + at.n - 1, share.total, share.ctas));
-  }
+  // the item that the CTA finds begun, for the kernel below: warp 0's share begins where the CTA's does
+  const int4 begun = make_int4(at.tile == 0 ? -1 : at.s, (at.hk * p.G + at.cut * p.gh) | min(p.gh, p.G - at.cut * p.gh) << 24, share.begin - at.tile,
+                               share.begin - at.tile + at.n - 1);
+  auto write_found = [&]() {
+    if (threadIdx.x == 0)
+      p.found[blockIdx.x] = begun.x < 0 ? begun
+                                        : make_int4(begun.x, begun.y, share.cuts.cta_of(begun.z), share.cuts.cta_of(begun.w));
+  };
   const int count = share.count;
   if (count > 0) {
     // the item that is summed, and how many items this warp has begun, on the copying side and on this one
@@ -569,6 +601,7 @@ decode_kernel(const DecodeParams p) {
       begin_values(ring + (2 * i + 1) * kDecTileBytes, there);
     }
 
+    write_found();
     Queries<HT> q, q_next;
     int h0, heads, next_no = 0;      // q_next: queries of item next_no of this warp, if that is ahead of item_no
     auto heads_of = [&](int k, int c) {
@@ -634,6 +667,8 @@ decode_kernel(const DecodeParams p) {
       sm.put(reinterpret_cast<float*>(ring_bytes), kDecRow, reinterpret_cast<float2*>(ring_bytes + HT * 8 * kDecRow * 4));
       if (lane == 0) pieces[2 * warp + 1] = {kPieceThere | (item_begin >= 0 ? kPieceBegins : 0), s, h0 | heads << 24};
     }
+  } else {
+    write_found();
   }
   pdl_trigger();      // see join_kernel
   __syncthreads();
@@ -652,9 +687,9 @@ constexpr int kJoinThreads = 256;
 template <int HT>
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const DecodeParams p) {
+  constexpr int kColumns = HT * 8 * kHeadDim / 4;
   __shared__ float4 sums[kJoinThreads];
   __shared__ float2 mls[kJoinThreads];
-  constexpr int kColumns = HT * 8 * kHeadDim / 4;
   pdl_wait();
   const int4 found = p.found[blockIdx.x];
   if (found.x < 0) return;
@@ -665,39 +700,41 @@ join_kernel(const DecodeParams p) {
   const int heads = found.y >> 24, h0 = found.y & 0xffffff;
   const int lanes = min(width, kJoinThreads), groups = kJoinThreads / lanes;
   const int group = threadIdx.x / lanes, lane = threadIdx.x - group * lanes;
+  float top, sum;
+  float4 acc;
+  auto add = [&](const float2& ml, const float4& o) {
+    const float high = fmaxf(top, ml.x), base = exp_base(high);
+    const float f = fast_exp2(top - base), w = fast_exp2(ml.x - base);
+    top = high;
+    sum = sum * f + ml.y * w;
+    acc.x = acc.x * f + o.x * w; acc.y = acc.y * f + o.y * w; acc.z = acc.z * f + o.z * w; acc.w = acc.w * f + o.w * w;
+  };
   for (int column = rank * width + lane; column < (rank + 1) * width; column += lanes) {      // once but for strips wider than the CTA
     const int head = column / (kHeadDim / 4);
-    float top = -INFINITY, sum = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    top = -INFINITY;
+    sum = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (head < heads) {
 #pragma unroll 4
       for (int i = group; i <= sharers; i += groups) {      // piece 0 in slot 2 c0 + 1, piece i in slot 2 (c0 + i)
         const int64_t slot = i == 0 ? 2 * c0 + 1 : 2 * (c0 + i);
-        const float2 ml = p.part_ml[slot * (HT * 8) + head];
-        const float4 o = *reinterpret_cast<const float4*>(p.part_o + slot * (HT * 8 * kHeadDim) + 4 * column);
-        const float high = fmaxf(top, ml.x), base = exp_base(high);
-        const float f = fast_exp2(top - base), w = fast_exp2(ml.x - base);
-        top = high;
-        sum = sum * f + ml.y * w;
-        acc.x = acc.x * f + o.x * w; acc.y = acc.y * f + o.y * w; acc.z = acc.z * f + o.z * w; acc.w = acc.w * f + o.w * w;
+        add(p.part_ml[slot * (HT * 8) + head], *reinterpret_cast<const float4*>(p.part_o + slot * (HT * 8 * kHeadDim) + 4 * column));
       }
     }
-    for (int half = groups / 2; half > 0; half /= 2) {
+    // the groups of a warp, then those of the warps
+    for (int o = lanes; o < 32; o *= 2) {
+      const float2 ml = make_float2(__shfl_down_sync(0xffffffffu, top, o), __shfl_down_sync(0xffffffffu, sum, o));
+      add(ml, make_float4(__shfl_down_sync(0xffffffffu, acc.x, o), __shfl_down_sync(0xffffffffu, acc.y, o),
+                          __shfl_down_sync(0xffffffffu, acc.z, o), __shfl_down_sync(0xffffffffu, acc.w, o)));
+    }
+    if (groups > 1) {
+      const int apart = max(lanes, 32);
       __syncthreads();
-      if (group >= half && group < 2 * half) {
-        sums[threadIdx.x - half * lanes] = acc;
-        mls[threadIdx.x - half * lanes] = make_float2(top, sum);
-      }
+      sums[threadIdx.x] = acc;
+      mls[threadIdx.x] = make_float2(top, sum);
       __syncthreads();
-      if (group < half) {
-        const float2 ml = mls[threadIdx.x];
-        const float4 o = sums[threadIdx.x];
-        const float high = fmaxf(top, ml.x), base = exp_base(high);
-        const float f = fast_exp2(top - base), w = fast_exp2(ml.x - base);
-        top = high;
-        sum = sum * f + ml.y * w;
-        acc.x = acc.x * f + o.x * w; acc.y = acc.y * f + o.y * w; acc.z = acc.z * f + o.z * w; acc.w = acc.w * f + o.w * w;
-      }
+      if (group == 0)
+        for (int i = threadIdx.x + apart; i < kJoinThreads; i += apart) add(mls[i], sums[i]);
     }
     if (group == 0 && head < heads) {
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
@@ -754,9 +791,9 @@ extern "C" rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor 
   p.cuts = (p.G + 15) / 16;
   p.gh = (p.G + p.cuts - 1) / p.cuts;
   p.items = p.Hkv * p.cuts;
-  // heads share a word with a count, a warp counts its tiles in 31 bits
-  const long long most_tiles = static_cast<long long>(p.S) * p.items * (static_cast<long long>(p.max_pages) * p.P / kDecKeys + 1);
-  if (p.Hq >= 1 << 24 || most_tiles / (kDecCtas * kDecWarps) >= 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
+  // heads share a word with a count, units of work are counted in 31 bits
+  const double most_units = static_cast<double>(p.S) * p.items * (static_cast<double>(p.max_pages) * p.P / kDecKeys + 1 + kDecItemCost);
+  if (p.Hq >= 1 << 24 || most_units >= 2147483647.0) return RBS_ERR_UNSUPPORTED;
   const DecodeWorkspace ws = decode_workspace(p.G);
   if (workspace == nullptr || workspace_bytes < ws.bytes || reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return RBS_ERR_WORKSPACE;
   unsigned char* base = static_cast<unsigned char*>(workspace);
