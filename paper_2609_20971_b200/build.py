@@ -51,7 +51,7 @@ def build_native(force: bool = False) -> str:
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-shared",
                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
                     *(x for p in system for x in ("-isystem", p)), NATIVE_SOURCE, "-o", NATIVE, "-L", os.path.join(base, "lib"),
-                    "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
+                    "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"], check=True)
     return NATIVE
 
 

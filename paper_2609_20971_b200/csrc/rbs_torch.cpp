@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -125,7 +126,10 @@ class Call {
     r.magnitude = number(i + 6);
     return r;
   }
-  at::Tensor output(int i, const at::Tensor& like) { return given(i) ? tensor(i) : at::empty(like.sizes(), like.options().requires_grad(false)); }
+  at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type) const {
+    return at::detail::empty_cuda(sizes, type, c10::Device(c10::kCUDA, static_cast<c10::DeviceIndex>(device_)), std::nullopt);
+  }
+  at::Tensor output(int i, const at::Tensor& like) { return given(i) ? tensor(i) : fresh(like.sizes(), like.scalar_type()); }
 
   int small(int64_t v) const {
     if (v < -0x80000000ll || v > 0x7fffffffll) refuse("a size is outside 32 bits");
@@ -195,7 +199,7 @@ PyObject* extend(PyObject*, PyObject* const* args, Py_ssize_t n) {
     at::Tensor out[5];
     int* p[5];
     for (int i = 0; i < 5; ++i) {
-      out[i] = c.given(8 + i) ? c.tensor(8 + i) : at::empty({sizes[i]}, seq_lens.options().dtype(at::kInt));
+      out[i] = c.given(8 + i) ? c.tensor(8 + i) : c.fresh({sizes[i]}, at::kInt);
       p[i] = c.vector<int>(out[i], sizes[i]);
     }
     const int *lens = c.vector<int>(seq_lens, shape.n_seqs), *more = c.vector<int>(new_lens, shape.n_seqs);
@@ -271,13 +275,13 @@ PyObject* decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const rbs_tensor tq = c.rows(q, q.sizes()), to = c.rows(out, q.sizes());
     const int* l = c.vector<int>(lens, shape.n_seqs);
     at::Tensor lse, ws;
-    if (c.truth(6)) lse = at::empty({q.size(0), q.size(1)}, q.options().dtype(at::kFloat).requires_grad(false));
+    if (c.truth(6)) lse = c.fresh({q.size(0), q.size(1)}, at::kFloat);
     const float scale = c.number(7);
     if (c.given(8)) {
       ws = c.tensor(8);
       if (ws.scalar_type() != at::kByte || !ws.is_contiguous()) c.refuse("the workspace must be a contiguous uint8 tensor");
     } else {
-      ws = at::empty({static_cast<int64_t>(lib_decode_workspace(&shape))}, q.options().dtype(at::kByte).requires_grad(false));
+      ws = c.fresh({static_cast<int64_t>(lib_decode_workspace(&shape))}, at::kByte);
     }
     c.run([&](void* stream) {
       return lib_decode(&shape, tq, tk, tv, static_cast<const int*>(table.data_ptr()), l, to,
