@@ -30,6 +30,7 @@ struct RopeParams {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kRopeResident = 5;                 // CTAs of an SM
 constexpr int kRopeAhead = 4;                    // pairs of rows that a warp has in flight, in shared memory
 
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
@@ -154,7 +155,7 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
 // A CTA has 8 / spread tokens, `spread` warps for each.  Its threads compute the tokens' angles once, behind the first rows'
 // loads.
 template <bool INTERLEAVED, bool WHOLE, bool PAGED>
-__global__ void __launch_bounds__(kRopeThreads, 5)
+__global__ void __launch_bounds__(kRopeThreads, kRopeResident)
 rope_kernel(const RopeParams p) {
   __shared__ float2 angles[kRopeWarps][kHeadDim / 2];
   __shared__ __align__(16) unsigned char rings[kRopeWarps * kRopeAhead * 512];
@@ -282,11 +283,13 @@ static void set_rope(RopeParams& p, const rbs_rope* r) {
   p.eps = r->eps; p.magnitude = r->magnitude; p.rot = r->rot_dim;
 }
 
-// A token is spread over as many warps as leave all CTAs resident at a time, four per SM; one where that does not fit.
+// A token is spread over 8 or 4 warps where all CTAs are then resident at a time, over 2 up to two such waves, and stays with
+// one warp behind that: a spread shortens the row of pairs that a warp goes through, and costs the weights of each warp.  us with
+// 1 / 2 / 4 / 8 warps, 36 heads: 680 tokens 8.2 / 8.2 / 6.5 / 5.5; 1,003 8.5 / 7.7 / 7.2 / 8.8; 4,000 17.1 / 16.4 / 18.4 / 24.0; 16,000
+// 49.7 / 52.7 / 60.9 / 83.8.
 static rbs_status launch_rope(RopeParams p, long long tokens, bool interleaved, bool paged, cudaStream_t s) {
-  const long long room = 4ll * sm_count();
-  p.spread = kRopeWarps;
-  while (p.spread > 1 && (tokens * p.spread + kRopeWarps - 1) / kRopeWarps > room) p.spread /= 2;
+  const long long room = static_cast<long long>(kRopeResident) * sm_count() * kRopeWarps;
+  p.spread = tokens * 8 <= room ? 8 : tokens * 4 <= room ? 4 : tokens * 2 <= 2 * room ? 2 : 1;
   const long long per_cta = kRopeWarps / p.spread, ctas = (tokens + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
   p.tokens = tokens;
