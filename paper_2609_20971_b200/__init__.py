@@ -9,8 +9,9 @@ from .binding import (BlockStats, PagedStep, RbsError, alloc_stats, alloc_step, 
                       rbs_block_stats_box, rbs_device_status, rbs_mask_group_union, rbs_paged_decode, rbs_paged_extend, rbs_qk_norm_rope,
                       rbs_qk_norm_rope_paged, rbs_select, rbs_select_box, rbs_select_chunk, rbs_select_static, rbs_sparse_prefill,
                       rbs_sparse_prefill_chunk, rbs_sparse_prefill_grouped, workspace_bytes)
+from .paged import PagedCache, rope_frequencies
 
-__all__ = ["BlockStats", "PagedStep", "RbsError", "alloc_stats", "alloc_step", "load_library", "load_native", "paged_decode_workspace_bytes", "rbs_block_stats",
+__all__ = ["BlockStats", "PagedCache", "PagedStep", "RbsError", "alloc_stats", "alloc_step", "load_library", "load_native", "paged_decode_workspace_bytes", "rbs_block_stats",
            "rbs_block_stats_box", "rbs_device_status", "rbs_mask_group_union", "rbs_paged_decode", "rbs_paged_extend", "rbs_qk_norm_rope",
            "rbs_qk_norm_rope_paged", "rbs_select", "rbs_select_box", "rbs_select_chunk", "rbs_select_static", "rbs_sparse_prefill",
-           "rbs_sparse_prefill_chunk", "rbs_sparse_prefill_grouped", "workspace_bytes"]
+           "rbs_sparse_prefill_chunk", "rbs_sparse_prefill_grouped", "rope_frequencies", "workspace_bytes"]

@@ -11,8 +11,9 @@ import pytest
 import torch
 
 from oracle import serving_oracle as so
-from paper_2609_20971_b200 import (RbsError, alloc_step, paged_decode_workspace_bytes, rbs_device_status, rbs_paged_decode,
-                                   rbs_paged_extend, rbs_qk_norm_rope, rbs_qk_norm_rope_paged)
+from paper_2609_20971_b200 import (PagedCache, RbsError, alloc_step, paged_decode_workspace_bytes, rbs_device_status, rbs_paged_decode,
+                                   rbs_paged_extend, rbs_qk_norm_rope, rbs_qk_norm_rope_paged, rope_frequencies)
+from paper_2609_20971_b200.binding import rbs_prefill_varlen
 
 pytestmark = pytest.mark.gpu
 STEP = 2.0 ** -8
@@ -371,6 +372,91 @@ def test_calls_on_another_stream_and_in_a_replayed_graph():
     assert b.lens.tolist() == [n + 28 for n in start]
     _check_decode(got[1], got[2], got[0], b.k, b.v, b.table, b.lens)
     assert rbs_device_status() == 0
+
+
+def test_prompts_and_generated_tokens_of_a_paged_cache():
+    """Packed prompts through the cache and the prefill call, then tokens one by one, sequences that end and others that take their
+    pages.  A prompt's last row of dense prefill attention is what decode attention of that token gives; everything the
+    decode steps read is followed by the oracle's own norm, rotation and attention in 64 bits."""
+    hq, hkv, layers, page = 8, 2, 2, 16
+    lens = [130, 1, 300]
+    cache = PagedCache(layers, 60, page, hkv, len(lens), 50, "cuda")
+    freq, magnitude = rope_frequencies(128, 1e4, scaling="yarn", factor=4.0, trained_len=64)
+    w = torch.rand(2, 128, device="cuda") + 0.5
+    turn = {"q_norm": w[0], "k_norm": w[1], "magnitude": magnitude}
+    kept = [[[] for _ in lens] for _ in range(layers)]      # (key, value) rows of every sequence, in bf16
+
+    def tokens(seed, step, new, layer, out_k=None):
+        n = step.slots.shape[0]
+        x = _randn(seed + layer, n, hq + 2 * hkv, 128, scale=2.0)
+        q, k, v = x.split((hq, hkv, hkv), dim=1)
+        got = cache.write(layer, q, k, v, step, freq, out_k=out_k, **turn)
+        _check_turn(got, q, step.positions, freq, w[0], magnitude=magnitude)
+        keys, _ = rbs_qk_norm_rope(k, k, step.positions, freq, q_norm=w[1], k_norm=w[1], magnitude=magnitude)
+        _check_turn(keys, k, step.positions, freq, w[1], magnitude=magnitude)
+        row = 0
+        for s, m in enumerate(new):
+            kept[layer][s] += [(keys[i], v[i]) for i in range(row, row + m)]
+            row += m
+        return got, v
+
+    def check(layer, q, out, lse):
+        for s, rows in enumerate(kept[layer]):
+            assert int(cache.lens[s]) == len(rows)
+            if not rows:
+                assert bool((out[s] == 0).all() and (lse[s] == -np.inf).all())
+                continue
+            k, v = (_f64(torch.stack([r[i] for r in rows])[None]) for i in (0, 1))
+            o, l, size = so.decode(_f64(q[s:s + 1]), k, v, np.zeros((1, 1), int), [len(rows)])
+            assert (np.abs(_f64(out[s]) - o[0]) <= STEP * np.abs(o[0]) + (STEP + 1e-4) * size[0]).all()
+            assert np.abs(_f64(lse[s]) - l[0]).max() <= 1e-4
+
+    step = cache.extend(_ints(lens), sum(lens))
+    cu = np.concatenate(([0], np.cumsum(lens)))
+    for layer in range(layers):
+        k = torch.empty(sum(lens), hkv, 128, dtype=torch.bfloat16, device="cuda")
+        q, v = tokens(100, step, lens, layer, out_k=k)
+        prompt_out, _ = rbs_prefill_varlen(q, k, v.contiguous(), cu.tolist(), 64, alpha_base=1e-30, alpha_rescue=1e-30)      # every block
+        last = torch.tensor(cu[1:] - 1, device="cuda")
+        out, lse = cache.attend(layer, q[last].contiguous(), return_lse=True)
+        check(layer, q[last], out, lse)
+        # prefill attention is within 2e-2 (max) and 2e-3 (mean) of the exact value, decode attention nearer
+        gap = (prompt_out[last].float() - out.float()).abs()
+        assert gap.max() <= 3e-2 and gap.mean() <= 3e-3
+    seed = 200
+    for new in ([1, 1, 1], [1, 0, 1], [5, 1, 1], [1, 1, 1]):
+        step = cache.extend(_ints(new), sum(new) + 1)
+        pad = step.slots[sum(new):]
+        assert bool((pad == -1).all())
+        for layer in range(layers):
+            q, _ = tokens(seed, step, new, layer)
+            ends = (step.cu[1:] - 1).clamp(min=0).long()
+            out, lse = cache.attend(layer, q[ends].contiguous(), return_lse=True)
+            check(layer, q[ends], out, lse)
+        seed += 10
+    assert int(cache.used) == sum(-(-len(rows) // page) for rows in kept[0])
+    held = -(-len(kept[0][1]) // page)
+    cache.release([2, 0, 2])
+    for layer in range(layers):
+        kept[layer][0], kept[layer][2] = [], []
+    assert int((cache.free_pages >= 0).sum()) == 60 - held and int(cache.used) == 0
+    new = [700, 1, 150]      # the pages of the sequences that ended are needed
+    step = cache.extend(_ints(new), sum(new))
+    assert int(step.slots.min()) >= 0 and len(set(step.slots.tolist())) == sum(new)
+    for layer in range(layers):
+        q, _ = tokens(seed, step, new, layer)
+        ends = (step.cu[1:] - 1).long()
+        out, lse = cache.attend(layer, q[ends].contiguous(), return_lse=True)
+        check(layer, q[ends], out, lse)
+    n = len(kept[0][1])
+    left = 60 - sum(-(-len(rows) // page) for rows in kept[0])
+    fit = -(-n // page) * page - n + left * page      # what the begun page and the pages that are left can hold
+    step = cache.extend(_ints([0, 200, 0]), 200)      # more than that
+    assert 0 < fit < 200 and int(cache.used) > 60
+    assert bool((step.slots[:fit] >= 0).all()) and bool((step.slots[fit:] == -1).all())
+    cache.release([])
+    with pytest.raises(RbsError):
+        cache.release([3])
 
 
 def test_calls_refuse_what_does_not_fit_together():

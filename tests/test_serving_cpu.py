@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from oracle import serving_oracle as so
-from paper_2609_20971_b200 import RbsError, binding, rbs_paged_decode, rbs_paged_extend, rbs_qk_norm_rope
+from paper_2609_20971_b200 import RbsError, binding, rbs_paged_decode, rbs_paged_extend, rbs_qk_norm_rope, rope_frequencies
 from paper_2609_20971_b200.binding import RbsPagedShape, RbsRope, RbsTensor
 
 OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
@@ -193,3 +193,24 @@ def test_oracle_extend_gives_every_token_a_place_of_its_own():
     assert lens.tolist() == [9, 0, 5] and cu.tolist() == [0, 6, 6, 7]
     assert pos.tolist() == [3, 4, 5, 6, 7, 8, 4, 0, 0]
     assert slots.tolist() == [39, 0, 1, 2, 3, 4, 8, -1, -1]
+
+
+def test_rope_frequencies():
+    f, m = rope_frequencies(64, 1e4, device="cpu")
+    want = 1e4 ** (-np.arange(32) / 32)
+    assert m == 1.0 and f.dtype == torch.float32 and np.allclose(f.numpy(), want, rtol=1e-7)
+    assert np.allclose(rope_frequencies(64, 1e4, scaling="linear", factor=4.0, device="cpu")[0].numpy(), want / 4, rtol=1e-7)
+    ntk = rope_frequencies(64, 1e4, scaling="ntk", factor=4.0, device="cpu")[0].numpy()
+    assert np.isclose(ntk[0], want[0]) and np.isclose(ntk[-1], want[-1] / 4, rtol=1e-6)
+    yarn, m = rope_frequencies(64, 1e4, scaling="yarn", factor=4.0, trained_len=4096, device="cpu")
+    turns = 4096 * want / (2 * np.pi)
+    ratio = yarn.numpy() / want
+    assert np.isclose(m, 0.1 * np.log(4.0) + 1.0)
+    assert np.allclose(ratio[turns > 45], 1.0, rtol=1e-6) and np.allclose(ratio[turns < 0.7], 0.25, rtol=1e-6)
+    assert (np.diff(ratio) <= 1e-7).all()
+    for args in ((60, 1e4), (0, 1e4), (136, 1e4), (64, 1.0)):
+        with pytest.raises(RbsError):
+            rope_frequencies(*args, device="cpu")
+    for more in ({"scaling": "other"}, {"scaling": "yarn", "factor": 2.0}, {"factor": 0.5}):
+        with pytest.raises(RbsError):
+            rope_frequencies(64, 1e4, device="cpu", **more)
