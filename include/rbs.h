@@ -358,7 +358,8 @@ typedef struct {
 /*
  * Q_out, K_out = norm and rotation of Q [batch][n_tokens][n_q_heads][128] and K [batch][n_tokens][n_kv_heads][128], whose
  * tokens have the positions rope->positions (the same for every batch entry).  One launch.  An output may be its own input
- * (same pointer and strides); it must not overlap an input in another way.  Head counts: any positive ones.
+ * (same pointer and strides); it must not overlap an input in another way, nor itself (a batch stride of 0 is
+ * RBS_ERR_INVALID_ARG for the outputs of a batch).  Head counts: any positive ones.
  */
 RBS_API rbs_status rbs_qk_norm_rope(int batch, int n_tokens, int n_q_heads, int n_kv_heads, int head_dim, rbs_tensor Q,
                                     rbs_tensor K, const rbs_rope* rope, rbs_tensor Q_out, rbs_tensor K_out, void* stream);
@@ -379,14 +380,15 @@ RBS_API rbs_status rbs_qk_norm_rope_paged(const rbs_paged_shape* shape, int n_to
 /*
  * Attention of one new token of each sequence over the paged cache (the new token's own key and value stand in it already):
  *   O_s = sum_{t < n_s} softmax_t(q_s.k_t * scale) v_t      for every query head, n_s = seq_lens[s]
- * Q, O: row s = sequence s (stride_token, stride_head; stride_batch ignored).  bf16 inputs, fp32 accumulation and softmax, bf16
- * output.  n_s is taken into [0, max_pages*page_size]; tokens whose page lies outside [0, n_pages) are left out.
+ * Q, O: row s = sequence s (stride_token, stride_head; stride_batch ignored); O may be Q itself (same pointer and strides).  bf16
+ * inputs, fp32 accumulation and softmax, bf16 output.  n_s is taken into [0, max_pages*page_size]; tokens whose page lies outside [0, n_pages) are left out.
  * A sequence without a token gets zeros and lse = -inf.  lse (nullable): fp32 [S][Hq], natural-log-sum-exp of the scaled logits.
  * softmax_scale == 0 means 1/sqrt(d).  The work of all sequences is cut into equal pieces on the device (no
  * length is read on the host, so a captured graph follows them); a sequence that is cut is joined in a fixed order: a call
  * with the same lengths gives the same bits, a sequence in another batch agrees to rounding.
- * Workspace: rbs_paged_decode_workspace_bytes(shape) bytes, 256-byte aligned; calls that may run at the same time need
- * one each.
+ * Workspace: rbs_paged_decode_workspace_bytes(shape) bytes, 256-byte aligned (its size depends on the group size alone); calls that
+ * may run at the same time need one each.
+ * RBS_ERR_UNSUPPORTED where the table could hold 2^31 tiles of 16 tokens and more over all sequences and KV heads.
  */
 RBS_API size_t rbs_paged_decode_workspace_bytes(const rbs_paged_shape* shape);
 RBS_API rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor Q, rbs_tensor k_cache, rbs_tensor v_cache,

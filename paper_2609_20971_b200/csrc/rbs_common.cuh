@@ -77,6 +77,14 @@ int sm_count();
 // Device address, on the current device, of the status word that bounded waits report to (nullptr if it cannot be
 // obtained).  Looked up once per device, with that device current: an address taken on one GPU means nothing on another.
 unsigned int* device_status_ptr();
+// The same for kernels that wait on nothing and report only the debug build's index checks: nullptr in the release build.
+inline unsigned int* debug_status() {
+#ifdef RBS_DEBUG
+  return device_status_ptr();
+#else
+  return nullptr;
+#endif
+}
 // cudaFuncSetAttribute(MaxDynamicSharedMemorySize) only when this (kernel, device) has not yet been given at least
 // `bytes`: the attribute is per device and sticky, and the call is not free on the per-layer path.
 rbs_status ensure_dynamic_smem(const void* kernel, size_t bytes);

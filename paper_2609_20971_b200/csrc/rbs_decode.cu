@@ -9,6 +9,7 @@
 // the last item of a share can be in pieces; pieces of one item are joined by the thread block at its end, and by a second
 // kernel where an item goes on in other thread blocks.  All joins are in the order of the tokens.
 #include "rbs_common.cuh"
+#include "rbs_sm100.cuh"
 
 namespace rbs {
 
@@ -43,6 +44,7 @@ struct DecodeParams {
   // 2 CTAs + 3 c + w - 1: of the item that warp w > 0 of CTA c found begun and finished
   float* part_o;   // [..][128] sums
   float2* part_ml; // maxima in use (log2 units) and normalisers
+  unsigned int* status;   // of the debug build's checks
   int4* found;     // [CTA] the item that its share finds begun: sequence (-1: none), first head | heads << 24, CTAs of its begin and end
 };
 
@@ -91,11 +93,12 @@ struct Softmax {
     }
   }
 
-  // Scores of 16 keys; `valid`: a bit per key.  p: their probabilities against the maximum in use, as the B operand of P V
-  // (rounded to bf16, at most 2^-8 relative each; l sums them unrounded, so that lse does not see the rounding).  The maximum
-  // moves only when a score passes it by kDecSlack: probabilities of up to 2^8 round no worse, and a tile that leaves it
-  // alone has no exchange between lanes and no rescaling.
-  __device__ __forceinline__ void scores(const Queries<HT>& q, uint32_t ktile, uint32_t valid, float scale_log2, uint32_t (&p)[HT][2]) {
+  // Scores of 16 keys; `valid`: a bit per key.  p: their probabilities against the maximum in use, as the B operands of P V: each
+  // is split into two bf16 numbers, off by 2^-17 relative, so that the output sees no rounding but its own (error against
+  // 64 bits 1.7e-3 instead of 2.3e-3, for 0.3 - 0.8 % of the time).
+  // The maximum moves only when a score passes it by kDecSlack: probabilities of up to 2^8 round no worse, and a tile that
+  // leaves it alone has no exchange between lanes and no rescaling.
+  __device__ __forceinline__ void scores(const Queries<HT>& q, uint32_t ktile, uint32_t valid, float scale_log2, uint32_t (&p)[HT][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2;
     float c[HT][4];
 #pragma unroll
@@ -147,19 +150,26 @@ struct Softmax {
         c[n][i + 2] = fast_exp2(c[n][i + 2] - base);
         l[n][i] += c[n][i] + c[n][i + 2];
       }
-      p[n][0] = transpose_8x8(pack_bf16(c[n][0], c[n][1]));
-      p[n][1] = transpose_8x8(pack_bf16(c[n][2], c[n][3]));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t high = pack_bf16(c[n][2 * i], c[n][2 * i + 1]);
+        p[n][i] = transpose_8x8(high);
+        p[n][i + 2] = transpose_8x8(pack_bf16(c[n][2 * i] - bf16lo(high), c[n][2 * i + 1] - bf16hi(high)));
+      }
     }
   }
 
-  __device__ __forceinline__ void values(uint32_t vtile, const uint32_t (&p)[HT][2]) {
+  __device__ __forceinline__ void values(uint32_t vtile, const uint32_t (&p)[HT][4]) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       uint32_t a[4];
       ldmatrix_x4_trans(a[0], a[1], a[2], a[3], vtile + tile_off((lane & 7) + (lane >> 4) * 8, 2 * j + ((lane >> 3) & 1)));
 #pragma unroll
-      for (int n = 0; n < HT; ++n) mma_bf16_16816(o[n][j], a, p[n][0], p[n][1]);
+      for (int n = 0; n < HT; ++n) {
+        mma_bf16_16816(o[n][j], a, p[n][0], p[n][1]);
+        mma_bf16_16816(o[n][j], a, p[n][2], p[n][3]);
+      }
     }
   }
 
@@ -174,6 +184,7 @@ struct Softmax {
   }
   // O and lse of a whole item
   __device__ __forceinline__ void write(const DecodeParams& p, int s, int h0, int heads) const {
+    if (!RBS_DBG_OK(s >= 0 && s < p.S && h0 >= 0 && heads > 0 && h0 + heads <= p.Hq, p.status, kDbgDecodeRow)) return;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int n = 0; n < HT; ++n) {
@@ -484,6 +495,7 @@ __device__ __forceinline__ void join_pieces(const DecodeParams& p, const unsigne
     there &= ~mine;
     ended &= ~mine;
     const int s = pieces[first].s, h0 = pieces[first].h0_heads & 0xffffff, heads = pieces[first].h0_heads >> 24;
+    if (!RBS_DBG_OK(s >= 0 && s < p.S && h0 >= 0 && heads > 0 && h0 + heads <= p.Hq, p.status, kDbgDecodeRow)) continue;
 #pragma unroll
     for (int n = 0; n < HT; ++n) {
       const int h = 8 * n + (threadIdx.x >> 4), e = (threadIdx.x & 15) * 8;
@@ -626,7 +638,7 @@ decode_kernel(const DecodeParams p) {
       const uint32_t kt = ring + 2 * (i % kDecStages) * kDecTileBytes, vt = kt + kDecTileBytes;
       const uint32_t word = queue[0];
       queue[0] = queue[1];
-      uint32_t pr[HT][2];
+      uint32_t pr[HT][4];
       cp_async_wait<2 * kDecStages - 1>();
       __syncwarp();
       sm.scores(q, kt, word & 0xffffu, p.scale_log2, pr);
@@ -647,7 +659,8 @@ decode_kernel(const DecodeParams p) {
         sm.write(p, s, h0, heads);
       } else {
         const int64_t slot = warp == 0 ? 2 * blockIdx.x : 2 * kDecCtas + (kDecWarps - 1) * blockIdx.x + warp - 1;
-        sm.put(p.part_o + slot * (HT * 8) * kHeadDim, kHeadDim, p.part_ml + slot * (HT * 8));
+        if (RBS_DBG_OK(slot >= 0 && slot < kDecSlots, p.status, kDbgDecodeSlot))
+          sm.put(p.part_o + slot * (HT * 8) * kHeadDim, kHeadDim, p.part_ml + slot * (HT * 8));
         if (warp > 0 && lane == 0) pieces[2 * warp] = {kPieceThere | kPieceEnds, s, h0 | heads << 24};
       }
       item_begin = i + 1;
@@ -698,10 +711,11 @@ join_kernel(const DecodeParams p) {
   while (width * sharers < kColumns) width *= 2;
   if (rank * width >= kColumns) return;
   const int heads = found.y >> 24, h0 = found.y & 0xffffff;
+  if (!RBS_DBG_OK(found.x < p.S && heads > 0 && h0 + heads <= p.Hq && c0 >= 0 && found.w < kDecCtas, p.status, kDbgDecodeRow)) return;
   const int lanes = min(width, kJoinThreads), groups = kJoinThreads / lanes;
   const int group = threadIdx.x / lanes, lane = threadIdx.x - group * lanes;
   float top, sum;
-  float4 acc;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](const float2& ml, const float4& o) {
     const float high = fmaxf(top, ml.x), base = exp_base(high);
     const float f = fast_exp2(top - base), w = fast_exp2(ml.x - base);
@@ -785,6 +799,7 @@ extern "C" rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor 
   p.K = static_cast<const __nv_bfloat16*>(k_cache.ptr); p.kp = k_cache.stride_batch; p.kt = k_cache.stride_token; p.kh = k_cache.stride_head;
   p.V = static_cast<const __nv_bfloat16*>(v_cache.ptr); p.vp = v_cache.stride_batch; p.vt = v_cache.stride_token; p.vh = v_cache.stride_head;
   p.O = static_cast<__nv_bfloat16*>(O.ptr); p.ost = O.stride_token; p.osh = O.stride_head;
+  p.status = debug_status();
   p.lse = lse; p.table = block_table; p.lens = seq_lens;
   p.S = shape->n_seqs; p.Hq = shape->n_q_heads; p.Hkv = shape->n_kv_heads; p.G = p.Hq / p.Hkv;
   p.P = shape->page_size; p.n_pages = shape->n_pages; p.max_pages = shape->max_pages; p.stride = shape->table_stride;

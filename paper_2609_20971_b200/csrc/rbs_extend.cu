@@ -4,6 +4,7 @@
 // page p of sequence s, first_s <= p < last_s, is entry free_used + a_s + p - first_s of the free list.
 // Bound by its launch: a decode step of 64 sequences moves 2 KB, half a million prompt tokens 4.8 MB.
 #include "rbs_common.cuh"
+#include "rbs_sm100.cuh"
 
 namespace rbs {
 
@@ -25,6 +26,7 @@ struct ExtendParams {
   int* free_used_out;
   int S, P, n_pages, max_pages, stride, n_free, T;
   bool aligned;           // positions and slots take 16-byte stores
+  unsigned int* status;   // of the debug build's checks
 };
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -151,7 +153,8 @@ extend_kernel(const ExtendParams p) {
   }
   for (int k = me; k < fresh; k += step) {
     const int s = last_not_above(at, p.S, k);
-    p.table[static_cast<int64_t>(s) * p.stride + ceil_div(past[s], p.P) + k - at[s]] = free_page(k);
+    const int entry = ceil_div(past[s], p.P) + k - at[s];
+    if (RBS_DBG_OK(entry >= 0 && entry < p.max_pages, p.status, kDbgExtendEntry)) p.table[static_cast<int64_t>(s) * p.stride + entry] = free_page(k);
   }
   const int groups = p.T > 0 ? (p.T - 1) / ROWS + 1 : 0;
   for (int group = me; group < groups; group += step) {
@@ -245,6 +248,7 @@ extern "C" rbs_status rbs_paged_extend(const rbs_paged_shape* shape, const int* 
   p.free_used_out = free_used_out;
   p.S = shape->n_seqs; p.P = shape->page_size; p.n_pages = shape->n_pages; p.max_pages = shape->max_pages;
   p.stride = shape->table_stride; p.n_free = n_free; p.T = n_tokens;
+  p.status = debug_status();
   p.aligned = (reinterpret_cast<uintptr_t>(positions) | reinterpret_cast<uintptr_t>(slots)) % 16 == 0;
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
   if (p.S < kExtendFew && p.T <= kExtendFew) return launch_extend<kExtendFew, 1>(p, cs);

@@ -315,6 +315,7 @@ extern "C" rbs_status rbs_qk_norm_rope(int batch, int n_tokens, int n_q_heads, i
   if ((st = check_tensor(Q)) != RBS_OK || (st = check_tensor(K)) != RBS_OK || (st = check_tensor(Q_out)) != RBS_OK ||
       (st = check_tensor(K_out)) != RBS_OK)
     return st;
+  if (batch > 1 && (Q_out.stride_batch == 0 || K_out.stride_batch == 0)) return RBS_ERR_INVALID_ARG;
   RopeParams p = {};
   p.Q = static_cast<const __nv_bfloat16*>(Q.ptr); p.qsb = Q.stride_batch; p.qst = Q.stride_token; p.qsh = Q.stride_head;
   p.K = static_cast<const __nv_bfloat16*>(K.ptr); p.ksb = K.stride_batch; p.kst = K.stride_token; p.ksh = K.stride_head;

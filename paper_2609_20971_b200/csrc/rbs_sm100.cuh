@@ -115,6 +115,9 @@ enum DebugSite : unsigned int {
   kDbgPrefillTile = 8,     // attention: query tile outside this call's queries
   kDbgPrefillPart = 9,     // attention: partial-result slot outside the workspace
   kDbgPrefillLse = 10,     // attention: lse index past the end
+  kDbgExtendEntry = 11,    // extending sequences: block-table entry outside the sequence's row
+  kDbgDecodeRow = 12,      // decode attention: output row outside the sequences or the heads
+  kDbgDecodeSlot = 13,     // decode attention: piece of an item outside the workspace
 };
 #ifdef RBS_DEBUG
 __device__ __forceinline__ bool dbg_record(bool cond, unsigned int* status, unsigned int site) {

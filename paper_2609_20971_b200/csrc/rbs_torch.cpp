@@ -167,6 +167,14 @@ PyObject* guarded(F&& f) {
   return nullptr;
 }
 
+// n elements of a fresh 1-d tensor, from element `at` on, without the dispatcher
+at::Tensor part_of(const at::Tensor& whole, int64_t at, int64_t n) {
+  static const int64_t kOne = 1;
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+  t.unsafeGetTensorImpl()->set_sizes_and_strides(c10::IntArrayRef(&n, 1), c10::IntArrayRef(&kOne, 1), at);
+  return t;
+}
+
 PyObject* pack(std::initializer_list<at::Tensor> ts) {
   PyObject* out = PyTuple_New(static_cast<Py_ssize_t>(ts.size()));
   if (out == nullptr) return nullptr;
@@ -196,10 +204,15 @@ PyObject* extend(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int tokens = c.integer(6);
     if (tokens < 0) c.refuse("n_tokens is negative");
     const int64_t sizes[5] = {shape.n_seqs, shape.n_seqs + 1ll, tokens, tokens, 1};
-    at::Tensor out[5];
+    at::Tensor out[5], all;
     int* p[5];
-    for (int i = 0; i < 5; ++i) {
-      out[i] = c.given(8 + i) ? c.tensor(8 + i) : c.fresh({sizes[i]}, at::kInt);
+    if (!c.given(8)) {      // one allocation, 16-byte aligned parts
+      int64_t n = 0;
+      for (int64_t size : sizes) n += (size + 3) / 4 * 4;
+      all = c.fresh({n}, at::kInt);
+    }
+    for (int64_t i = 0, at = 0; i < 5; at += (sizes[i] + 3) / 4 * 4, ++i) {
+      out[i] = all.defined() ? part_of(all, at, sizes[i]) : c.tensor(static_cast<int>(8 + i));
       p[i] = c.vector<int>(out[i], sizes[i]);
     }
     const int *lens = c.vector<int>(seq_lens, shape.n_seqs), *more = c.vector<int>(new_lens, shape.n_seqs);

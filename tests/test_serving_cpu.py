@@ -93,6 +93,8 @@ def test_norm_rope_refuses_sizes(lib):
                                             (1, 5, 8, 0, 128, INVALID), (1, 5, 8, 2, 64, UNSUPPORTED)]:
         assert lib.rbs_qk_norm_rope(batch, tokens, hq, hkv, d, _t(), _t(), _turn(), _t(), _t(), None) == want
     assert lib.rbs_qk_norm_rope(1, 5, 8, 2, 128, _t(), _t(), None, _t(), _t(), None) == INVALID
+    for outs in ((_t(sb=0), _t(sb=640)), (_t(sb=640), _t(sb=0))):      # a batch that would be written over itself
+        assert lib.rbs_qk_norm_rope(2, 5, 8, 2, 128, _t(), _t(), _turn(), *outs, None) == INVALID
 
 
 @pytest.mark.parametrize("which", range(6))
@@ -136,6 +138,11 @@ def test_decode_refuses_tensors(lib, name, bad):
 @pytest.mark.parametrize("args", [dict(table=None), dict(lens=None), dict(scale=NAN), dict(scale=INF)])
 def test_decode_refuses_arguments(lib, args):
     assert _decode(lib, _shape(), **args) == INVALID
+
+
+def test_decode_refuses_tables_of_too_many_tiles(lib):
+    big = dict(n_seqs=1 << 13, n_q_heads=64, n_kv_heads=64, max_pages=1 << 17, table_stride=1 << 17)
+    assert _decode(lib, _shape(**big)) == UNSUPPORTED
 
 
 @pytest.mark.parametrize("args", [dict(ws=None), dict(ws=0x100080), dict(n=0), dict(n=-1)])
