@@ -30,8 +30,9 @@ struct RopeParams {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
-constexpr int kRopeResident = 5;                 // CTAs of an SM
-constexpr int kRopeAhead = 4;                    // pairs of rows that a warp has in flight, in shared memory
+constexpr int kRopeResident = 4;                 // CTAs of an SM
+constexpr int kRopeAhead = 2;                    // groups of rows that a warp has in flight, in shared memory
+constexpr int kRopeGroup = 2;                    // pairs of rows of a group: the shuffles of one pair fill the waits of the other
 
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   float2 d;
@@ -78,37 +79,50 @@ struct RopeLane {
       s[k] = make_float2(sj[2 * k], sj[2 * k + 1]);
     }
   }
-  // Two neighbouring elements at a time (packed fp32 instructions).
-  template <bool NORM>
-  __device__ __forceinline__ void turn(uint2& xa, uint2& xb) const {
-    const float2 x[4] = {make_float2(bf16lo(xa.x), bf16hi(xa.x)), make_float2(bf16lo(xa.y), bf16hi(xa.y)),
-                         make_float2(bf16lo(xb.x), bf16hi(xb.x)), make_float2(bf16lo(xb.y), bf16hi(xb.y))};
-    float2 y[4];
+  // Two neighbouring elements at a time (packed fp32 instructions), N rows side by side.
+  template <bool NORM, int N>
+  __device__ __forceinline__ void turn(uint2 (&xa)[N], uint2 (&xb)[N]) const {
+    float2 y[N][4];
+    float sum[N];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = mul2(x[k], c[k]);
-    if (WHOLE || turns) {      // elsewhere a zero would still carry an infinite neighbour over
+    for (int i = 0; i < N; ++i) {
+      const float2 x[4] = {make_float2(bf16lo(xa[i].x), bf16hi(xa[i].x)), make_float2(bf16lo(xa[i].y), bf16hi(xa[i].y)),
+                           make_float2(bf16lo(xb[i].x), bf16hi(xb[i].x)), make_float2(bf16lo(xb[i].y), bf16hi(xb[i].y))};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = fma2(INTERLEAVED ? make_float2(x[k].y, x[k].x) : x[k ^ 2], s[k], y[k]);
-    }
-    if (NORM) {
+      for (int k = 0; k < 4; ++k) y[i][k] = mul2(x[k], c[k]);
+      if (WHOLE || turns) {      // elsewhere a zero would still carry an infinite neighbour over
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[i][k] = fma2(INTERLEAVED ? make_float2(x[k].y, x[k].x) : x[k ^ 2], s[k], y[i][k]);
+      }
       float2 ss = mul2(x[0], x[0]);
 #pragma unroll
       for (int k = 1; k < 4; ++k) ss = fma2(x[k], x[k], ss);
-      float sum = ss.x + ss.y;
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      const float r = rsqrtf(sum * (1.0f / kHeadDim) + eps);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = mul2(y[k], make_float2(r, r));
+      sum[i] = ss.x + ss.y;
     }
-    xa = make_uint2(pack_bf16(y[0].x, y[0].y), pack_bf16(y[1].x, y[1].y));
-    xb = make_uint2(pack_bf16(y[2].x, y[2].y), pack_bf16(y[3].x, y[3].y));
+    if (NORM) {
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float r = rsqrtf(sum[i] * (1.0f / kHeadDim) + eps);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[i][k] = mul2(y[i][k], make_float2(r, r));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      xa[i] = make_uint2(pack_bf16(y[i][0].x, y[i][0].y), pack_bf16(y[i][1].x, y[i][1].y));
+      xb[i] = make_uint2(pack_bf16(y[i][2].x, y[i][2].y), pack_bf16(y[i][3].x, y[i][3].y));
+    }
   }
 };
 
-// The rows of one warp, two heads at a time, in order: its heads of Q, of K, of V.  kRopeAhead pairs are on their way to a ring of
-// its own in shared memory (in registers they would cost as many as the arithmetic).  All but the second head of a last pair
-// is the same for both halves, so that the warp stays together: halves that went through loops of their own took twice the
+// The rows of one warp, two heads at a time, in order: its heads of Q, of K, of V.  kRopeAhead groups of kRopeGroup such pairs are on
+// their way to a ring of its own in shared memory (in registers they would cost as many as the arithmetic; pair by pair a
+// chunk of 8,191 tokens of 64 heads takes 59.8 us instead of 57.7, 128K tokens of 32 heads 386 instead of 392).  All but the
+// second head of a last pair is the same for both halves, so that the warp stays together: halves that went through loops of their own took twice the
 // instructions (447 us instead of 367 for 128K tokens of 36 heads).
 struct RopeRows {
   const __nv_bfloat16* at;       // this half's row that is fetched next, at this lane's 16 bytes
@@ -119,16 +133,18 @@ struct RopeRows {
 
   template <typename Open>
   __device__ __forceinline__ void fetch(Open& open) {
-    if (left > 0) {
-      if (head < heads) cp_async16_zfill(ring + fill + (threadIdx.x & 15) * 16, at, true);
+    if (left <= 0 && kind < 2) open(*this, kind + 1);
+#pragma unroll
+    for (int j = 0; j < kRopeGroup; ++j) {
+      if (j < left && head < heads) cp_async16_zfill(ring + fill + j * 512 + (threadIdx.x & 15) * 16, at, true);
       at += skip;
       head += step;
-      if (--left == 0) open(*this, kind + 1);
     }
+    left -= kRopeGroup;
     cp_async_commit();
-    fill = fill == (kRopeAhead - 1) * 512 ? 0 : fill + 512;
+    fill = fill == (kRopeAhead - 1) * kRopeGroup * 512 ? 0 : fill + kRopeGroup * 512;
   }
-  // the next pair has arrived: the address of this half's row
+  // the next group has arrived: the address of this half's row of its first pair
   __device__ __forceinline__ uint32_t wait() {
     cp_async_wait<kRopeAhead - 1>();
     __syncwarp();
@@ -137,7 +153,7 @@ struct RopeRows {
   template <typename Open>
   __device__ __forceinline__ void done(Open& open) {
     __syncwarp();
-    read = read == (kRopeAhead - 1) * 512 ? 0 : read + 512;
+    read = read == (kRopeAhead - 1) * kRopeGroup * 512 ? 0 : read + kRopeGroup * 512;
     fetch(open);
   }
 };
@@ -158,7 +174,7 @@ template <bool INTERLEAVED, bool WHOLE, bool PAGED>
 __global__ void __launch_bounds__(kRopeThreads, kRopeResident)
 rope_kernel(const RopeParams p) {
   __shared__ float2 angles[kRopeWarps][kHeadDim / 2];
-  __shared__ __align__(16) unsigned char rings[kRopeWarps * kRopeAhead * 512];
+  __shared__ __align__(16) unsigned char rings[kRopeWarps * kRopeAhead * kRopeGroup * 512];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), u = threadIdx.x & 15, side = (threadIdx.x >> 4) & 1;
   const int per_cta = kRopeWarps / p.spread, mine = warp / p.spread, pair0 = warp - mine * p.spread, h0 = 2 * pair0 + side;
   const long long token0 = static_cast<long long>(blockIdx.x) * per_cta, token = token0 + mine;
@@ -169,6 +185,18 @@ rope_kernel(const RopeParams p) {
   lane.eps = p.eps;
   pdl_trigger();
   pdl_wait();
+  // What is needed behind the first rows' arrival is asked for before them: the frequency and the position of this thread's first
+  // angle, and the norms' weights (to L2).
+  const int k = threadIdx.x & (kHeadDim / 2 - 1), first = threadIdx.x / (kHeadDim / 2);
+  const unsigned t0 = static_cast<unsigned>(token0 < p.N ? token0 : token0 % p.N);
+  auto position = [&](int i) { return p.positions[t0 + i < static_cast<unsigned>(p.N) ? t0 + i : (t0 + i) % p.N]; };
+  const bool angle = k < p.rot / 2 && first < per_cta && token0 + first < p.tokens;
+  const float freq = angle ? p.inv_freq[k] : 0.f;
+  int pos = angle ? position(first) : 0;
+  if (p.spread > 1 && threadIdx.x < 2 * kHeadDim * 4 / 128) {
+    const float* w = threadIdx.x & 1 ? p.k_norm : p.q_norm;
+    if (w != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(w + (threadIdx.x >> 1) * 32));
+  }
   const bool live = token < p.tokens;
   const int64_t l = token < p.N ? 0 : token / p.N, t = token - l * p.N;
   __nv_bfloat16 *kc = nullptr, *vc = nullptr;
@@ -201,7 +229,7 @@ rope_kernel(const RopeParams p) {
   RopeRows rows;
   rows.step = step;
   rows.left = 0;
-  rows.ring = smem_u32(rings) + warp * kRopeAhead * 512 + side * 256;
+  rows.ring = smem_u32(rings) + warp * kRopeAhead * kRopeGroup * 512 + side * 256;
   rows.fill = rows.read = 0;
   open(rows, 0);
 #pragma unroll
@@ -209,19 +237,18 @@ rope_kernel(const RopeParams p) {
 
   // Angles in revolutions, as fractions of 2^64: positions are whole numbers, so whole revolutions of the frequency drop out of
   // the product by themselves, and an angle is off by 2^-33 of a revolution at most however far the position is.
-  const int k = threadIdx.x & (kHeadDim / 2 - 1);
-  if (k < p.rot / 2) {
-    double f = static_cast<double>(p.inv_freq[k]) * 0.15915494309189535;
+  if (angle) {
+    double f = static_cast<double>(freq) * 0.15915494309189535;
     f = (f - floor(f)) * 18446744073709551616.0;
     const unsigned long long each = __double2ull_rn(f);
-    const unsigned t0 = static_cast<unsigned>(token0 < p.N ? token0 : token0 % p.N);
-    for (int i = threadIdx.x / (kHeadDim / 2); i < per_cta && token0 + i < p.tokens; i += kRopeThreads / (kHeadDim / 2)) {
-      const unsigned at = t0 + i;
-      const long long pos = p.positions[at < static_cast<unsigned>(p.N) ? at : at % p.N];
+    for (int i = first;;) {
       float sn, cs;
-      sincospif(static_cast<float>(static_cast<int>(static_cast<unsigned long long>(pos) * each >> 32)) * 4.656612873077393e-10f, &sn,
-                &cs);      // 2^-31: in half revolutions
+      sincospif(static_cast<float>(static_cast<int>(static_cast<unsigned long long>(static_cast<long long>(pos)) * each >> 32)) *
+                    4.656612873077393e-10f, &sn, &cs);      // 2^-31: in half revolutions
       angles[i][k] = make_float2(cs * p.magnitude, sn * p.magnitude);
+      i += kRopeThreads / (kHeadDim / 2);
+      if (i >= per_cta || token0 + i >= p.tokens) break;
+      pos = position(i);
     }
   }
   __syncthreads();
@@ -233,17 +260,26 @@ rope_kernel(const RopeParams p) {
     *reinterpret_cast<uint2*>(row + lane.b) = xb;
   };
   auto turn_rows = [&](auto norm, int n, int heads, __nv_bfloat16* dst, int64_t skip, __nv_bfloat16* dst2, int64_t skip2) {
-    for (int i = 0, h = h0; i < n; ++i, h += step) {
+    for (int i = 0, h = h0; i < n; i += kRopeGroup) {
       const uint32_t from = rows.wait();
-      uint2 xa = lds64(from + at_a), xb = lds64(from + at_b);
+      uint2 xa[kRopeGroup], xb[kRopeGroup];
+#pragma unroll
+      for (int j = 0; j < kRopeGroup; ++j) {      // a pair that is not there is turned and not written
+        xa[j] = lds64(from + j * 512 + at_a);
+        xb[j] = lds64(from + j * 512 + at_b);
+      }
       rows.done(open);
       lane.template turn<decltype(norm)::value>(xa, xb);
-      if (h < heads) {
-        if (!PAGED || dst != nullptr) put(dst, xa, xb);
-        if (PAGED && dst2 != nullptr) put(dst2, xa, xb);
+#pragma unroll
+      for (int j = 0; j < kRopeGroup; ++j) {
+        if (i + j < n && h < heads) {
+          if (!PAGED || dst != nullptr) put(dst, xa[j], xb[j]);
+          if (PAGED && dst2 != nullptr) put(dst2, xa[j], xb[j]);
+        }
+        if (!PAGED || dst != nullptr) dst += skip;
+        if (PAGED && dst2 != nullptr) dst2 += skip2;
+        h += step;
       }
-      if (!PAGED || dst != nullptr) dst += skip;
-      if (PAGED && dst2 != nullptr) dst2 += skip2;
     }
   };
   if (n_q > 0) {
@@ -260,10 +296,15 @@ rope_kernel(const RopeParams p) {
     else turn_rows(std::false_type(), n_k, p.Hkv, out, step * p.kosh, out2, step * p.kch);
   }
   if (PAGED) {
-    for (int i = 0, h = h0; i < n_v; ++i, h += step) {
-      const uint4 x = lds128(rows.wait() + u * 16);
+    for (int i = 0, h = h0; i < n_v; i += kRopeGroup) {
+      const uint32_t from = rows.wait() + u * 16;
+      uint4 x[kRopeGroup];
+#pragma unroll
+      for (int j = 0; j < kRopeGroup; ++j) x[j] = lds128(from + j * 512);
       rows.done(open);
-      if (h < p.Hkv) *reinterpret_cast<uint4*>(vc + h * p.vch + 8 * u) = x;
+#pragma unroll
+      for (int j = 0; j < kRopeGroup; ++j, h += step)
+        if (i + j < n_v && h < p.Hkv) *reinterpret_cast<uint4*>(vc + h * p.vch + 8 * u) = x[j];
     }
   }
 }
@@ -283,13 +324,12 @@ static void set_rope(RopeParams& p, const rbs_rope* r) {
   p.eps = r->eps; p.magnitude = r->magnitude; p.rot = r->rot_dim;
 }
 
-// A token is spread over 8 or 4 warps where all CTAs are then resident at a time, over 2 up to two such waves, and stays with
-// one warp behind that: a spread shortens the row of pairs that a warp goes through, and costs the weights of each warp.  us with
-// 1 / 2 / 4 / 8 warps, 36 heads: 680 tokens 8.2 / 8.2 / 6.5 / 5.5; 1,003 8.5 / 7.7 / 7.2 / 8.8; 4,000 17.1 / 16.4 / 18.4 / 24.0; 16,000
-// 49.7 / 52.7 / 60.9 / 83.8.
+// A token is spread over as many of 8, 4, 2 warps as leave all CTAs resident at a time, and stays with one warp where that does not
+// fit: a spread shortens the row of pairs that a warp goes through, and costs the weights of each warp.  us with 1 / 2 / 4 / 8 warps,
+// 36 heads: 400 tokens 6.6 / 5.5 / 5.2 / 4.8; 1,003 8.9 / 8.4 / 6.9 / 9.1; 2,000 11.9 / 10.0 / 12.0 / 14.9; 4,000 15.5 / 17.1 / 20.0 / 27.1.
 static rbs_status launch_rope(RopeParams p, long long tokens, bool interleaved, bool paged, cudaStream_t s) {
   const long long room = static_cast<long long>(kRopeResident) * sm_count() * kRopeWarps;
-  p.spread = tokens * 8 <= room ? 8 : tokens * 4 <= room ? 4 : tokens * 2 <= 2 * room ? 2 : 1;
+  p.spread = tokens * 8 <= room ? 8 : tokens * 4 <= room ? 4 : tokens * 2 <= room ? 2 : 1;
   const long long per_cta = kRopeWarps / p.spread, ctas = (tokens + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
   p.tokens = tokens;
