@@ -315,7 +315,7 @@ static rbs_status check_rope(const rbs_rope* r, int n_tokens) {
   if (r->rot_dim < 0 || (r->interleaved != 0 && r->interleaved != 1)) return RBS_ERR_INVALID_ARG;
   if (r->rot_dim > kHeadDim || r->rot_dim % 8 != 0) return RBS_ERR_UNSUPPORTED;
   if (r->rot_dim > 0 && r->inv_freq == nullptr) return RBS_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(r->q_norm) % 16 != 0 || reinterpret_cast<uintptr_t>(r->k_norm) % 16 != 0) return RBS_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(r->q_norm) % 4 != 0 || reinterpret_cast<uintptr_t>(r->k_norm) % 4 != 0) return RBS_ERR_INVALID_ARG;
   return RBS_OK;
 }
 

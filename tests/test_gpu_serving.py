@@ -297,6 +297,18 @@ def test_decode_of_more_sequences_than_one_chunk_of_the_search():
     _check_decode(out, lse, q, k, v, table, n)
 
 
+def test_decode_of_sequences_that_share_their_pages():
+    """A common prompt: 330 block tables name the same pages, 58 thousand tiles of work over 0.7 MB of keys.  That much work goes to
+    two waves of thread blocks."""
+    k, v, table, _ = _sequences(25, [2900], 16, 1)
+    lens = [2900 - 3 * (i % 50) for i in range(330)]
+    table = table.expand(330, -1).contiguous()
+    q = _randn(26, 330, 3, 128, scale=1.5)
+    assert sum(-(-n // 16) + 2 for n in lens) > 444 * 4 * 32
+    out, lse = rbs_paged_decode(q, k, v, table, _ints(lens), return_lse=True)
+    _check_decode(out, lse, q, k, v, table, _ints(lens))
+
+
 def test_decode_leaves_out_tokens_whose_page_does_not_exist():
     k, v, table, lens = _sequences(11, [300, 40, 64], 16, 2)
     q = _randn(12, 3, 8, 128)
