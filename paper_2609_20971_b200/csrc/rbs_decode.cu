@@ -384,18 +384,18 @@ struct Share {
   int count;         // this warp's tiles
 };
 
-// Finds this warp's share and the place where it begins.  A chunk of four lengths per thread at a time; up to 512 sequences are one
-// chunk and are read once.
+// Finds this warp's share and the place where it begins, four lengths per thread at a time.  Up to 128 sequences every warp
+// reads and searches them alone; more are searched by the CTA, up to 512 of them at a time, which are read once if that is all.
+// (One sequence of 4,001 tokens: 10.0 us, 10.2 with the CTA's search.)
 __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
   __shared__ unsigned part[kDecWarps];
-  __shared__ uint4 found[kDecWarps + 1];      // where warp w's share begins: sequence, its length, unit within it, next length
+  __shared__ uint4 shared_found[kDecWarps + 1];
   constexpr int kChunk = kDecWarps * 32 * 4;
   const int warp = threadIdx.x >> 5;
   int len[5];
   unsigned n[4];
-  auto load = [&](int base) {
+  auto load = [&](int s) {      // lengths s .. s + 4, units of sequences s .. s + 3; their sum
     unsigned sum = 0;
-    const int s = base + threadIdx.x * 4;
 #pragma unroll
     for (int i = 0; i < 5; ++i) len[i] = read_len(p, s + i);
 #pragma unroll
@@ -405,41 +405,81 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
     }
     return sum;
   };
-  unsigned total = 0, sum = 0, before = 0;
-  if (p.S <= kChunk) {
-    before = scan_cta(load(0), part, &total);
-  } else {
-    for (int base = 0; base < p.S; base += kChunk) sum += load(base);
-    scan_cta(sum, part, &total);
-  }
   Share sh;
-  sh.cuts.set(total);
   sh.begin = 0;
   sh.count = 0;
-  const unsigned c = blockIdx.x;
-  if (c >= sh.cuts.ctas) return sh;
-  const unsigned begin = sh.cuts.begin(c), units = sh.cuts.begin(c + 1) - begin;
-  unsigned seen = 0;
-  for (int base = 0; base < p.S; base += kChunk) {
-    if (p.S > kChunk) before = scan_cta(load(base), part, &total);
-    unsigned first = seen + before;
+  unsigned begin, units;
+  uint4 f, g;      // where this warp's share begins and the next one's: sequence, its length, unit within it, length of the one behind
+  auto my_share = [&](unsigned total) {      // of the CTA; false if it has none
+    sh.cuts.set(total);
+    if (blockIdx.x >= sh.cuts.ctas) return false;
+    begin = sh.cuts.begin(blockIdx.x);
+    units = sh.cuts.begin(blockIdx.x + 1) - begin;
+    return true;
+  };
+  const uint4 behind_all = make_uint4(p.S, 0, 0, 0);
+  if (p.S <= 128) {
+    const int lane = threadIdx.x & 31;
+    const unsigned sum = load(lane * 4);
+    unsigned x = sum;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int w = 0; w <= kDecWarps; ++w) {
-        const unsigned in = begin + units * w / kDecWarps - first;      // wraps where the sequence lies behind
-        if (in < n[i]) found[w] = make_uint4(base + threadIdx.x * 4 + i, len[i], in, len[i + 1]);
-      }
-      first += n[i];
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
     }
-    seen += total;
-    if (begin + units < seen) break;
+    if (!my_share(__shfl_sync(0xffffffffu, x, 31))) return sh;
+    auto find = [&](unsigned want) {
+      uint4 mine = behind_all;
+      unsigned first = x - sum;
+      bool here = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (want - first < n[i]) {      // wraps where the sequence lies behind
+          mine = make_uint4(lane * 4 + i, len[i], want - first, len[i + 1]);
+          here = true;
+        }
+        first += n[i];
+      }
+      const unsigned who = __ballot_sync(0xffffffffu, here);
+      const int from = who != 0 ? __ffs(who) - 1 : 0;
+      const uint4 r = make_uint4(__shfl_sync(0xffffffffu, mine.x, from), __shfl_sync(0xffffffffu, mine.y, from),
+                                 __shfl_sync(0xffffffffu, mine.z, from), __shfl_sync(0xffffffffu, mine.w, from));
+      return who != 0 ? r : behind_all;
+    };
+    f = find(begin + units * warp / kDecWarps);
+    g = find(begin + units * (warp + 1) / kDecWarps);
+  } else {
+    unsigned total = 0, sum = 0, before = 0;
+    if (p.S <= kChunk) {
+      before = scan_cta(load(threadIdx.x * 4), part, &total);
+    } else {
+      for (int base = 0; base < p.S; base += kChunk) sum += load(base + threadIdx.x * 4);
+      scan_cta(sum, part, &total);
+    }
+    if (!my_share(total)) return sh;
+    unsigned seen = 0;
+    for (int base = 0; base < p.S; base += kChunk) {
+      if (p.S > kChunk) before = scan_cta(load(base + threadIdx.x * 4), part, &total);
+      unsigned first = seen + before;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int w = 0; w <= kDecWarps; ++w) {
+          const unsigned in = begin + units * w / kDecWarps - first;
+          if (in < n[i]) shared_found[w] = make_uint4(base + threadIdx.x * 4 + i, len[i], in, len[i + 1]);
+        }
+        first += n[i];
+      }
+      seen += total;
+      if (begin + units < seen) break;
+    }
+    if (begin + units == sh.cuts.total && threadIdx.x == 0) shared_found[kDecWarps] = behind_all;
+    __syncthreads();
+    f = shared_found[warp];
+    g = shared_found[warp + 1];
   }
-  if (begin + units == sh.cuts.total && threadIdx.x == 0) found[kDecWarps] = make_uint4(p.S, 0, 0, 0);      // the end of all work
-  __syncthreads();
   // tiles in front of the place: units without those of the items' ends
-  auto place = [&](int w, Place& x) {
-    const uint4 f = found[w];
+  auto place = [&](const uint4& f, int w, Place& x) {
     x.s = f.x;
     x.len = clamped(p, f.y);
     x.next_len = f.w;
@@ -450,8 +490,8 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
     return begin + units * w / kDecWarps - max(x.tile - x.n, 0) - (x.s * p.items + x.item) * kDecItemCost;
   };
   Place end;
-  const unsigned last = place(warp + 1, end);
-  sh.count = last - place(warp, at);
+  const unsigned last = place(g, warp + 1, end);
+  sh.count = last - place(f, warp, at);
   sh.begin = begin + units * warp / kDecWarps;
   at.hk = p.cuts == 1 ? at.item : at.item / p.cuts;
   at.cut = at.item - at.hk * p.cuts;

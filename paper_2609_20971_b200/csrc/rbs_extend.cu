@@ -11,7 +11,8 @@ namespace rbs {
 constexpr int kExtendThreads = 1024;
 constexpr int kExtendFew = 256;         // threads where there is little to do: barriers of fewer warps are shorter
 constexpr int kExtendMaxSeqs = 8192;
-constexpr int kExtendRows = 8;          // token rows of a thread, one after the other, in large calls
+constexpr int kExtendRows = 4;          // token rows of a thread, one after the other (a 16-byte store), in large calls
+constexpr int kExtendGroups = 2;        // and how many times, a warp's width apart
 
 struct ExtendParams {
   const int* seq_lens;
@@ -78,10 +79,10 @@ __device__ __forceinline__ int last_not_above(const int* a, int n, int v) {
 }
 
 // Every CTA scans all lengths for itself (from L2, into shared memory), so that nothing is handed from CTA to CTA; then the
-// CTAs share out the sequences, the new table entries and the token rows.  One CTA per SM and rows one after the other in a
-// thread where there are many (1.2 million rows of 301 prompts: 7.5 us; two CTAs per SM with half the rows for each thread 10.3);
-// one row per thread otherwise (a decode step of 64 sequences: 2.9 us, 4.9 with 8 rows).
-template <int THREADS, int ROWS>
+// CTAs share out the sequences, the new table entries and the token rows.  One CTA per SM and 16-byte stores where there are many
+// rows (1.2 million rows of 301 prompts: 8.0 us, of which the scan 2.5; two CTAs per SM 10.3; eight rows one after the other, whose
+// stores leave gaps, 8.7); one row per thread otherwise (a decode step of 64 sequences: 2.8 us, 4.9 with eight).
+template <int THREADS, int ROWS, int GROUPS>
 __global__ void __launch_bounds__(THREADS)
 extend_kernel(const ExtendParams p) {
   extern __shared__ int shared[];
@@ -156,70 +157,76 @@ extend_kernel(const ExtendParams p) {
     const int entry = ceil_div(past[s], p.P) + k - at[s];
     if (RBS_DBG_OK(entry >= 0 && entry < p.max_pages, p.status, kDbgExtendEntry)) p.table[static_cast<int64_t>(s) * p.stride + entry] = free_page(k);
   }
-  const int groups = p.T > 0 ? (p.T - 1) / ROWS + 1 : 0;
-  for (int group = me; group < groups; group += step) {
-    const int row0 = group * ROWS;
-    int pos[ROWS], slot[ROWS];
-    int s = -1, behind = 0, page = -1, off = 0, index = 0, first = 0;
-    bool good = false;
+  const int lane = threadIdx.x & 31;
+  for (long long warp_row = static_cast<long long>(me >> 5) * (32 * ROWS * GROUPS); warp_row < p.T; warp_row += static_cast<long long>(step) * ROWS * GROUPS) {
+    int s = -1, behind = 0;      // the sequence of the last row, and the first row behind it
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int row = row0 + i;
-      pos[i] = 0;
-      slot[i] = -1;
-      if (row >= n_new) continue;
-      bool look = false;
-      if (row >= behind) {      // the first row, or the first one of another sequence
-        if (s < 0) s = last_not_above(cu, p.S, row);
-        else do ++s; while (cu[s + 1] <= row);
-        behind = cu[s + 1];
-        pos[i] = past[s] + row - cu[s];
-        index = pos[i] / p.P;
-        off = pos[i] - index * p.P;
-        first = ceil_div(past[s], p.P);
-        look = true;
-      } else {
-        pos[i] = i > 0 ? pos[i - 1] + 1 : 0;
-        if (++off == p.P) {
-          off = 0;
-          ++index;
-          look = true;
-        }
-      }
-      if (look) {
-        page = -1;
-        if (pos[i] < cap)      // the page that the sequence had begun, or a new one
-          page = index < first ? begun[s] : free_page(at[s] + index - first);
-        good = page >= 0 && page < p.n_pages;
-      }
-      if (good && pos[i] < cap) slot[i] = page * p.P + off;
-    }
-    if (ROWS % 4 == 0 && p.aligned && row0 + ROWS <= p.T) {
-#pragma unroll
-      for (int i = 0; i + 3 < ROWS; i += 4) {
-        *reinterpret_cast<int4*>(p.positions + row0 + i) = make_int4(pos[i], pos[i + 1], pos[i + 2], pos[i + 3]);
-        *reinterpret_cast<int4*>(p.slots + row0 + i) = make_int4(slot[i], slot[i + 1], slot[i + 2], slot[i + 3]);
-      }
-    } else {
+    for (int g = 0; g < GROUPS; ++g) {
+      const long long row64 = warp_row + (g * 32 + lane) * ROWS;
+      if (row64 >= p.T) break;
+      const int row0 = static_cast<int>(row64);
+      int pos[ROWS], slot[ROWS];
+      int page = -1, off = 0, index = 0, first = 0;
+      bool good = false, begin = true;      // begin: position and page are worked out, not counted on
 #pragma unroll
       for (int i = 0; i < ROWS; ++i) {
-        if (row0 + i < p.T) {
-          p.positions[row0 + i] = pos[i];
-          p.slots[row0 + i] = slot[i];
+        const int row = row0 + i;
+        pos[i] = 0;
+        slot[i] = -1;
+        if (row >= n_new) continue;
+        if (row >= behind) {
+          if (begin) s = last_not_above(cu, p.S, row);
+          else do ++s; while (cu[s + 1] <= row);
+          behind = cu[s + 1];
+          begin = true;
+        }
+        bool look = begin;
+        if (begin) {
+          pos[i] = past[s] + row - cu[s];
+          index = pos[i] / p.P;
+          off = pos[i] - index * p.P;
+          first = ceil_div(past[s], p.P);
+          begin = false;
+        } else {
+          pos[i] = pos[i > 0 ? i - 1 : 0] + 1;
+          if (++off == p.P) {
+            off = 0;
+            ++index;
+            look = true;
+          }
+        }
+        if (look) {
+          page = -1;
+          if (pos[i] < cap)      // the page that the sequence had begun, or a new one
+            page = index < first ? begun[s] : free_page(at[s] + index - first);
+          good = page >= 0 && page < p.n_pages;
+        }
+        if (good && pos[i] < cap) slot[i] = page * p.P + off;
+      }
+      if (ROWS == 4 && p.aligned && row0 + ROWS <= p.T) {
+        *reinterpret_cast<int4*>(p.positions + row0) = make_int4(pos[0], pos[1 % ROWS], pos[2 % ROWS], pos[3 % ROWS]);
+        *reinterpret_cast<int4*>(p.slots + row0) = make_int4(slot[0], slot[1 % ROWS], slot[2 % ROWS], slot[3 % ROWS]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+          if (row0 + i < p.T) {
+            p.positions[row0 + i] = pos[i];
+            p.slots[row0 + i] = slot[i];
+          }
         }
       }
     }
   }
 }
 
-template <int THREADS, int ROWS>
+template <int THREADS, int ROWS, int GROUPS>
 static rbs_status launch_extend(const ExtendParams& p, cudaStream_t stream) {
   const size_t smem = (4 * static_cast<size_t>(p.S) + 2) * sizeof(int);
-  const rbs_status st = ensure_dynamic_smem(reinterpret_cast<const void*>(extend_kernel<THREADS, ROWS>), smem);
+  const rbs_status st = ensure_dynamic_smem(reinterpret_cast<const void*>(extend_kernel<THREADS, ROWS, GROUPS>), smem);
   if (st != RBS_OK) return st;
-  const int groups = p.T > 0 ? (p.T - 1) / ROWS + 1 : 0, work = groups > p.S + 1 ? groups : p.S + 1;
+  const int groups = p.T > 0 ? (p.T - 1) / (ROWS * GROUPS) + 1 : 0, work = groups > p.S + 1 ? groups : p.S + 1;
   const int ctas = (work - 1) / THREADS + 1, most = sm_count();
-  RBS_CUDA_OK(launch_pdl(extend_kernel<THREADS, ROWS>, static_cast<unsigned>(ctas < most ? ctas : most), 1, THREADS, smem, stream, p));
+  RBS_CUDA_OK(launch_pdl(extend_kernel<THREADS, ROWS, GROUPS>, static_cast<unsigned>(ctas < most ? ctas : most), 1, THREADS, smem, stream, p));
   return RBS_OK;
 }
 
@@ -251,6 +258,6 @@ extern "C" rbs_status rbs_paged_extend(const rbs_paged_shape* shape, const int* 
   p.status = debug_status();
   p.aligned = (reinterpret_cast<uintptr_t>(positions) | reinterpret_cast<uintptr_t>(slots)) % 16 == 0;
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  if (p.S < kExtendFew && p.T <= kExtendFew) return launch_extend<kExtendFew, 1>(p, cs);
-  return p.T <= sm_count() * kExtendThreads ? launch_extend<kExtendThreads, 1>(p, cs) : launch_extend<kExtendThreads, kExtendRows>(p, cs);
+  if (p.S < kExtendFew && p.T <= kExtendFew) return launch_extend<kExtendFew, 1, 1>(p, cs);
+  return p.T <= sm_count() * kExtendThreads ? launch_extend<kExtendThreads, 1, 1>(p, cs) : launch_extend<kExtendThreads, kExtendRows, kExtendGroups>(p, cs);
 }
