@@ -327,9 +327,11 @@ static void set_rope(RopeParams& p, const rbs_rope* r) {
 // A token is spread over as many of 8, 4, 2 warps as leave all CTAs resident at a time, and stays with one warp where that does not
 // fit: a spread shortens the row of pairs that a warp goes through, and costs the weights of each warp.  us with 1 / 2 / 4 / 8 warps,
 // 36 heads: 400 tokens 6.6 / 5.5 / 5.2 / 4.8; 1,003 8.9 / 8.4 / 6.9 / 9.1; 2,000 11.9 / 10.0 / 12.0 / 14.9; 4,000 15.5 / 17.1 / 20.0 / 27.1.
+// Where a token has many rows two warps go on paying for four times as many (80 rows: 4,000 tokens 33.3 / 30.6, 8,000 56.7 / 55.7).
 static rbs_status launch_rope(RopeParams p, long long tokens, bool interleaved, bool paged, cudaStream_t s) {
   const long long room = static_cast<long long>(kRopeResident) * sm_count() * kRopeWarps;
-  p.spread = tokens * 8 <= room ? 8 : tokens * 4 <= room ? 4 : tokens * 2 <= room ? 2 : 1;
+  const bool many = p.Hq + p.Hkv * (paged ? 2 : 1) >= 64;
+  p.spread = tokens * 8 <= room ? 8 : tokens * 4 <= room ? 4 : tokens * 2 <= (many ? 4 : 1) * room ? 2 : 1;
   const long long per_cta = kRopeWarps / p.spread, ctas = (tokens + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
   p.tokens = tokens;
