@@ -863,7 +863,9 @@ extern "C" rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor 
   const size_t smem = static_cast<size_t>(kDecWarps) * kDecRing;
   if ((st = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem)) != RBS_OK) return st;
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  RBS_CUDA_OK(launch_pdl(kernel, kDecCtas, 1, kDecWarps * 32, smem, cs, p));
-  RBS_CUDA_OK(launch_pdl(p.gh <= 8 ? join_kernel<1> : join_kernel<2>, kDecCtas, 1, kJoinThreads, 0, cs, p));
+  // no more CTAs than the table could have work for (four units each)
+  const unsigned ctas = static_cast<unsigned>(most_units / kDecWarps + 1 < kDecCtas ? most_units / kDecWarps + 1 : kDecCtas);
+  RBS_CUDA_OK(launch_pdl(kernel, ctas, 1, kDecWarps * 32, smem, cs, p));
+  RBS_CUDA_OK(launch_pdl(p.gh <= 8 ? join_kernel<1> : join_kernel<2>, ctas, 1, kJoinThreads, 0, cs, p));
   return RBS_OK;
 }

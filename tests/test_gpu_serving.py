@@ -494,6 +494,25 @@ def test_prompts_and_generated_tokens_of_a_paged_cache():
         cache.release([3])
 
 
+def test_calls_on_two_streams_at_once():
+    """Two streams issue decode steps side by side, each with its own sequences; nothing is shared but the library."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    cases = []
+    for i, (lens, hq, hkv, page) in enumerate((([3000, 20, 700], 32, 4, 64), ([100] * 50 + [5000], 16, 2, 24))):
+        k, v, table, n = _sequences(30 + i, lens, page, hkv)
+        q = _randn(40 + i, len(lens), hq, 128)
+        cases.append((q, k, v, table, n, rbs_paged_decode(q, k, v, table, n)))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(40):
+        for side, (q, k, v, table, n, _) in zip(range(2), cases):
+            with torch.cuda.stream(streams[side]):
+                got[side].append(rbs_paged_decode(q, k, v, table, n))
+    torch.cuda.synchronize()
+    for side in range(2):
+        assert all(torch.equal(out, cases[side][5]) for out in got[side])
+
+
 def test_calls_refuse_what_does_not_fit_together():
     q, cache, table, lens = _randn(1, 2, 8, 128), _randn(2, 3, 16, 2, 128), _ints([[0], [1]]), _ints([3, 4])
     pos, freq = _ints([0, 1]), _frequencies(128)
