@@ -733,7 +733,7 @@ constexpr int kJoinThreads = 256;
 // Joins the pieces of the items that lie in several CTAs' shares.  The CTAs that found an item begun share out its 1024 * HT
 // sums: the more pieces, the narrower the strip of each, so that every CTA reads about as much as one piece holds.  Thread
 // (group, column) takes four sums of every groups-th piece, with the maximum as it goes, so that all its loads can be on
-// their way together; the groups are joined in order.  The order depends on the lengths alone.
+// their way together; the groups are joined in order, maxima first.  The order depends on the lengths alone.
 // It becomes resident at the end of the kernel above, and lets no later kernel do so before its own end: the kernel above fills
 // every SM exactly, and where waiting CTAs had taken places of its own its last CTAs started late (64 sequences of 64 heads:
 // 239 us instead of 218 with triggers at both kernels' begins).
@@ -747,48 +747,71 @@ join_kernel(const DecodeParams p) {
   const int4 found = p.found[blockIdx.x];
   if (found.x < 0) return;
   const int c0 = found.z, sharers = found.w - c0, rank = blockIdx.x - c0 - 1;
-  int width = 4;      // columns of a strip
-  while (width * sharers < kColumns) width *= 2;
+  // columns of a strip: a power of two, at least a quarter of a warp's 16-byte loads
+  const int fair = (kColumns + sharers - 1) / sharers;
+  const int width = fair <= 4 ? 4 : 1 << (32 - __clz(fair - 1));
   if (rank * width >= kColumns) return;
   const int heads = found.y >> 24, h0 = found.y & 0xffffff;
   if (!RBS_DBG_OK(found.x < p.S && heads > 0 && h0 + heads <= p.Hq && c0 >= 0 && found.w < kDecCtas, p.status, kDbgDecodeRow)) return;
-  const int lanes = min(width, kJoinThreads), groups = kJoinThreads / lanes;
-  const int group = threadIdx.x / lanes, lane = threadIdx.x - group * lanes;
-  float top, sum;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](const float2& ml, const float4& o) {
-    const float high = fmaxf(top, ml.x), base = exp_base(high);
-    const float f = fast_exp2(top - base), w = fast_exp2(ml.x - base);
-    top = high;
-    sum = sum * f + ml.y * w;
-    acc.x = acc.x * f + o.x * w; acc.y = acc.y * f + o.y * w; acc.z = acc.z * f + o.z * w; acc.w = acc.w * f + o.w * w;
-  };
+  const int lanes = min(width, kJoinThreads), shift = __ffs(lanes) - 1, groups = kJoinThreads >> shift;      // powers of two
+  const int group = threadIdx.x >> shift, lane = threadIdx.x & (lanes - 1), apart = max(lanes, 32);
   for (int column = rank * width + lane; column < (rank + 1) * width; column += lanes) {      // once but for strips wider than the CTA
     const int head = column / (kHeadDim / 4);
-    top = -INFINITY;
-    sum = 0.f;
-    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float top = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto fade = [&](float high) {      // everything against the maximum `high` from here on
+      const float f = fast_exp2(top - exp_base(high));
+      top = high;
+      sum *= f;
+      acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+    };
     if (head < heads) {
 #pragma unroll 4
       for (int i = group; i <= sharers; i += groups) {      // piece 0 in slot 2 c0 + 1, piece i in slot 2 (c0 + i)
         const int64_t slot = i == 0 ? 2 * c0 + 1 : 2 * (c0 + i);
-        add(p.part_ml[slot * (HT * 8) + head], *reinterpret_cast<const float4*>(p.part_o + slot * (HT * 8 * kHeadDim) + 4 * column));
+        const float2 ml = p.part_ml[slot * (HT * 8) + head];
+        const float4 o = *reinterpret_cast<const float4*>(p.part_o + slot * (HT * 8 * kHeadDim) + 4 * column);
+        fade(fmaxf(top, ml.x));
+        const float w = fast_exp2(ml.x - exp_base(top));
+        sum = fmaf(ml.y, w, sum);
+        acc.x = fmaf(o.x, w, acc.x); acc.y = fmaf(o.y, w, acc.y); acc.z = fmaf(o.z, w, acc.z); acc.w = fmaf(o.w, w, acc.w);
       }
     }
-    // the groups of a warp, then those of the warps
-    for (int o = lanes; o < 32; o *= 2) {
-      const float2 ml = make_float2(__shfl_down_sync(0xffffffffu, top, o), __shfl_down_sync(0xffffffffu, sum, o));
-      add(ml, make_float4(__shfl_down_sync(0xffffffffu, acc.x, o), __shfl_down_sync(0xffffffffu, acc.y, o),
-                          __shfl_down_sync(0xffffffffu, acc.z, o), __shfl_down_sync(0xffffffffu, acc.w, o)));
+    // the groups of a warp, then those of the warps: first the maximum, then plain sums
+    if (lanes < 32) {
+      float high = top;
+      for (int o = lanes; o < 32; o *= 2) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+      fade(high);
+      for (int o = lanes; o < 32; o *= 2) {
+        sum += __shfl_down_sync(0xffffffffu, sum, o);
+        acc.x += __shfl_down_sync(0xffffffffu, acc.x, o);
+        acc.y += __shfl_down_sync(0xffffffffu, acc.y, o);
+        acc.z += __shfl_down_sync(0xffffffffu, acc.z, o);
+        acc.w += __shfl_down_sync(0xffffffffu, acc.w, o);
+      }
     }
     if (groups > 1) {
-      const int apart = max(lanes, 32);
       __syncthreads();
       sums[threadIdx.x] = acc;
       mls[threadIdx.x] = make_float2(top, sum);
       __syncthreads();
-      if (group == 0)
-        for (int i = threadIdx.x + apart; i < kJoinThreads; i += apart) add(mls[i], sums[i]);
+      if (group == 0) {
+        float high = top;
+#pragma unroll
+        for (int k = 1; k < kJoinThreads / 32; ++k)
+          if (threadIdx.x + k * apart < kJoinThreads) high = fmaxf(high, mls[threadIdx.x + k * apart].x);
+        fade(high);
+#pragma unroll
+        for (int k = 1; k < kJoinThreads / 32; ++k) {
+          const int i = threadIdx.x + k * apart;
+          if (i >= kJoinThreads) break;
+          const float2 ml = mls[i];
+          const float4 o = sums[i];
+          const float w = fast_exp2(ml.x - exp_base(high));
+          sum = fmaf(ml.y, w, sum);
+          acc.x = fmaf(o.x, w, acc.x); acc.y = fmaf(o.y, w, acc.y); acc.z = fmaf(o.z, w, acc.z); acc.w = fmaf(o.w, w, acc.w);
+        }
+      }
     }
     if (group == 0 && head < heads) {
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
