@@ -229,6 +229,7 @@ struct Place {
   int s, item, tile, n, len, next_len;   // n: tiles of an item of sequence s; next_len: length of sequence s + 1, as it was read
   int hk, cut;                           // of the item
   int page, in_page;                     // of the tile: entry of the table row, tile within the page (where pages hold whole tiles)
+  unsigned unit;                         // of all work (see Cuts)
 };
 
 __device__ __forceinline__ int read_len(const DecodeParams& p, int s) { return s < p.S ? p.lens[s] : 0; }
@@ -241,7 +242,9 @@ __device__ __forceinline__ bool step(const DecodeParams& p, Place& at) {
     at.in_page = 0;
     ++at.page;
   }
+  ++at.unit;
   if (++at.tile < at.n) return false;
+  at.unit += kDecItemCost;
   at.tile = at.page = at.in_page = 0;
   if (++at.cut == p.cuts) {
     at.cut = 0;
@@ -380,8 +383,7 @@ __device__ __forceinline__ unsigned scan_cta(unsigned v, unsigned* part, unsigne
 
 struct Share {
   Cuts cuts;
-  unsigned begin;    // unit of this warp's first tile
-  int count;         // this warp's tiles
+  unsigned end;      // the unit where this warp's share ends
 };
 
 // Finds this warp's share and the place where it begins, four lengths per thread at a time.  Up to 128 sequences every warp
@@ -389,7 +391,7 @@ struct Share {
 // (One sequence of 4,001 tokens: 10.0 us, 10.2 with the CTA's search.)
 __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
   __shared__ unsigned part[kDecWarps];
-  __shared__ uint4 shared_found[kDecWarps + 1];
+  __shared__ uint4 shared_found[kDecWarps];
   constexpr int kChunk = kDecWarps * 32 * 4;
   const int warp = threadIdx.x >> 5;
   int len[5];
@@ -406,10 +408,9 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
     return sum;
   };
   Share sh;
-  sh.begin = 0;
-  sh.count = 0;
+  sh.end = at.unit = 0;
   unsigned begin, units;
-  uint4 f, g;      // where this warp's share begins and the next one's: sequence, its length, unit within it, length of the one behind
+  uint4 f;      // where this warp's share begins: sequence, its length, unit within it, length of the one behind it
   auto my_share = [&](unsigned total) {      // of the CTA; false if it has none
     sh.cuts.set(total);
     if (blockIdx.x >= sh.cuts.ctas) return false;
@@ -417,7 +418,6 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
     units = sh.cuts.begin(blockIdx.x + 1) - begin;
     return true;
   };
-  const uint4 behind_all = make_uint4(p.S, 0, 0, 0);
   if (p.S <= 128) {
     const int lane = threadIdx.x & 31;
     const unsigned sum = load(lane * 4);
@@ -428,26 +428,20 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
       if (lane >= o) x += y;
     }
     if (!my_share(__shfl_sync(0xffffffffu, x, 31))) return sh;
-    auto find = [&](unsigned want) {
-      uint4 mine = behind_all;
-      unsigned first = x - sum;
-      bool here = false;
+    const unsigned want = begin + units * warp / kDecWarps;
+    unsigned first = x - sum;
+    bool here = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (want - first < n[i]) {      // wraps where the sequence lies behind
-          mine = make_uint4(lane * 4 + i, len[i], want - first, len[i + 1]);
-          here = true;
-        }
-        first += n[i];
+    for (int i = 0; i < 4; ++i) {
+      if (want - first < n[i]) {      // wraps where the sequence lies behind
+        f = make_uint4(lane * 4 + i, len[i], want - first, len[i + 1]);
+        here = true;
       }
-      const unsigned who = __ballot_sync(0xffffffffu, here);
-      const int from = who != 0 ? __ffs(who) - 1 : 0;
-      const uint4 r = make_uint4(__shfl_sync(0xffffffffu, mine.x, from), __shfl_sync(0xffffffffu, mine.y, from),
-                                 __shfl_sync(0xffffffffu, mine.z, from), __shfl_sync(0xffffffffu, mine.w, from));
-      return who != 0 ? r : behind_all;
-    };
-    f = find(begin + units * warp / kDecWarps);
-    g = find(begin + units * (warp + 1) / kDecWarps);
+      first += n[i];
+    }
+    const int from = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+    f = make_uint4(__shfl_sync(0xffffffffu, f.x, from), __shfl_sync(0xffffffffu, f.y, from), __shfl_sync(0xffffffffu, f.z, from),
+                   __shfl_sync(0xffffffffu, f.w, from));
   } else {
     unsigned total = 0, sum = 0, before = 0;
     if (p.S <= kChunk) {
@@ -464,7 +458,7 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int w = 0; w <= kDecWarps; ++w) {
+        for (int w = 0; w < kDecWarps; ++w) {
           const unsigned in = begin + units * w / kDecWarps - first;
           if (in < n[i]) shared_found[w] = make_uint4(base + threadIdx.x * 4 + i, len[i], in, len[i + 1]);
         }
@@ -473,31 +467,23 @@ __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
       seen += total;
       if (begin + units < seen) break;
     }
-    if (begin + units == sh.cuts.total && threadIdx.x == 0) shared_found[kDecWarps] = behind_all;
     __syncthreads();
     f = shared_found[warp];
-    g = shared_found[warp + 1];
   }
-  // tiles in front of the place: units without those of the items' ends
-  auto place = [&](const uint4& f, int w, Place& x) {
-    x.s = f.x;
-    x.len = clamped(p, f.y);
-    x.next_len = f.w;
-    x.n = tiles_of(x.len);
-    const unsigned cost = x.n + kDecItemCost;
-    x.item = f.z / cost;
-    x.tile = f.z - x.item * cost;
-    return begin + units * w / kDecWarps - max(x.tile - x.n, 0) - (x.s * p.items + x.item) * kDecItemCost;
-  };
-  Place end;
-  const unsigned last = place(g, warp + 1, end);
-  sh.count = last - place(f, warp, at);
-  sh.begin = begin + units * warp / kDecWarps;
+  sh.end = begin + units * (warp + 1) / kDecWarps;
+  at.unit = begin + units * warp / kDecWarps;
+  at.s = f.x;
+  at.len = clamped(p, f.y);
+  at.next_len = f.w;
+  at.n = tiles_of(at.len);
+  const unsigned cost = at.n + kDecItemCost;
+  at.item = f.z / cost;
+  at.tile = f.z - at.item * cost;
   at.hk = p.cuts == 1 ? at.item : at.item / p.cuts;
   at.cut = at.item - at.hk * p.cuts;
   at.page = at.in_page = 0;
   if (at.tile >= at.n) {      // the end of an item: on to the next one
-    sh.begin += at.n + kDecItemCost - at.tile;
+    at.unit += at.n - 1 - at.tile;      // its last tile, from where a step leads there
     at.tile = at.n - 1;
     at.in_page = -1;
     step(p, at);
@@ -607,37 +593,35 @@ decode_kernel(const DecodeParams p) {
     return;
   }
   // the item that the CTA finds begun, for the kernel below: warp 0's share begins where the CTA's does
-  const int4 begun = make_int4(at.tile == 0 ? -1 : at.s, (at.hk * p.G + at.cut * p.gh) | min(p.gh, p.G - at.cut * p.gh) << 24, share.begin - at.tile,
-                               share.begin - at.tile + at.n - 1);
+  const int4 begun = make_int4(at.tile == 0 ? -1 : at.s, (at.hk * p.G + at.cut * p.gh) | min(p.gh, p.G - at.cut * p.gh) << 24, at.unit - at.tile,
+                               at.unit - at.tile + at.n - 1);
   auto write_found = [&]() {
     if (threadIdx.x == 0)
       p.found[blockIdx.x] = begun.x < 0 ? begun
                                         : make_int4(begun.x, begun.y, share.cuts.cta_of(begun.z), share.cuts.cta_of(begun.w));
   };
-  const int count = share.count;
-  if (count > 0) {
+  if (at.unit < share.end) {
     // the item that is summed, and how many items this warp has begun, on the copying side and on this one
     int s = at.s, hk = at.hk, cut = at.cut, item = at.item;
-    int item_begin = at.tile == 0 ? 0 : -1;      // tile of the share, -1: before it
+    bool begun_here = at.tile == 0, finished = false;
     int copied_items = 0, item_no = 0;
 
     // tiles i + 1 and i + 2 are on their way while tile i is worked on, the table entry of tile i + 3 as well
     Lookup look = look_up<WHOLE>(p, at);
     TileSource<WHOLE> source;
-    int ahead = 0;
-    uint32_t queue[kDecStages];      // bits 0 - 15: the keys that there are, 16: last tile of its item
+    uint32_t queue[kDecStages];      // a word per tile, 0 behind the last one: bits 0 - 15: the keys that there are
+    constexpr uint32_t kTile = 0x20000u, kLast = 0x10000u;      // there is a tile; it is the last one of its item
     auto begin_keys = [&](uint32_t tile) {
       uint32_t word = 0;
-      if (ahead < count) {
+      if (at.unit < share.end) {
         source.set(p, look);
         source.template copy<false>(p, tile);
-        ++ahead;
         const bool last = step(p, at);
-        if (ahead < count) {
+        if (at.unit < share.end) {
           look = look_up<WHOLE>(p, at);
           copied_items += last;
         }
-        word = source.valid | (last ? 0x10000u : 0u);
+        word = kTile | source.valid | (last ? kLast : 0u);
       }
       cp_async_commit();
       return word;
@@ -648,9 +632,8 @@ decode_kernel(const DecodeParams p) {
     };
 #pragma unroll
     for (int i = 0; i < kDecStages; ++i) {
-      const bool there = ahead < count;
       queue[i] = begin_keys(ring + 2 * i * kDecTileBytes);
-      begin_values(ring + (2 * i + 1) * kDecTileBytes, there);
+      begin_values(ring + (2 * i + 1) * kDecTileBytes, queue[i] != 0);
     }
 
     write_found();
@@ -674,7 +657,7 @@ decode_kernel(const DecodeParams p) {
     fetch_next();
     Softmax<HT> sm;
     sm.start();
-    for (int i = 0; i < count; ++i) {
+    for (int i = 0; queue[0] != 0; ++i) {
       const uint32_t kt = ring + 2 * (i % kDecStages) * kDecTileBytes, vt = kt + kDecTileBytes;
       const uint32_t word = queue[0];
       queue[0] = queue[1];
@@ -683,19 +666,19 @@ decode_kernel(const DecodeParams p) {
       __syncwarp();
       sm.scores(q, kt, word & 0xffffu, p.scale_log2, pr);
       __syncwarp();
-      const bool more = ahead < count;
       queue[1] = begin_keys(kt);
       fetch_next();
       cp_async_wait<2 * kDecStages - 1>();
       __syncwarp();
       sm.values(vt, pr);
       __syncwarp();
-      begin_values(vt, more);
-      if (!(word & 0x10000u)) continue;
+      begin_values(vt, queue[1] != 0);
+      finished = word & kLast;
+      if (!finished) continue;
 
       // the end of the item
       sm.finish();
-      if (item_begin >= 0) {
+      if (begun_here) {
         sm.write(p, s, h0, heads);
       } else {
         const int64_t slot = warp == 0 ? 2 * blockIdx.x : 2 * kDecCtas + (kDecWarps - 1) * blockIdx.x + warp - 1;
@@ -703,11 +686,11 @@ decode_kernel(const DecodeParams p) {
           sm.put(p.part_o + slot * (HT * 8) * kHeadDim, kHeadDim, p.part_ml + slot * (HT * 8));
         if (warp > 0 && lane == 0) pieces[2 * warp] = {kPieceThere | kPieceEnds, s, h0 | heads << 24};
       }
-      item_begin = i + 1;
+      begun_here = true;
       ++item_no;
       if (++cut == p.cuts) { cut = 0; ++hk; }
       if (++item == p.items) { item = hk = 0; ++s; }
-      if (i + 1 < count) {
+      if (queue[0] != 0) {
         heads_of(hk, cut);
         if (next_no == item_no) q = q_next;
         else q.load(p.Q + s * p.qst + h0 * p.qsh, p.qsh, heads), next_no = item_no;
@@ -715,10 +698,10 @@ decode_kernel(const DecodeParams p) {
         sm.start();
       }
     }
-    if (item_begin < count) {      // an item is left unfinished
+    if (!finished) {      // an item is left unfinished
       sm.finish();
       sm.put(reinterpret_cast<float*>(ring_bytes), kDecRow, reinterpret_cast<float2*>(ring_bytes + HT * 8 * kDecRow * 4));
-      if (lane == 0) pieces[2 * warp + 1] = {kPieceThere | (item_begin >= 0 ? kPieceBegins : 0), s, h0 | heads << 24};
+      if (lane == 0) pieces[2 * warp + 1] = {kPieceThere | (begun_here ? kPieceBegins : 0), s, h0 | heads << 24};
     }
   } else {
     write_found();
