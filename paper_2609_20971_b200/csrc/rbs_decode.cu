@@ -388,7 +388,7 @@ struct Share {
 
 // Finds this warp's share and the place where it begins, four lengths per thread at a time.  Up to 128 sequences every warp
 // reads and searches them alone; more are searched by the CTA, up to 512 of them at a time, which are read once if that is all.
-// (One sequence of 4,001 tokens: 10.0 us, 10.2 with the CTA's search.)
+// (One sequence of 4,001 tokens: 0.25 us less than with the CTA's search.)
 __device__ __forceinline__ Share find_share(const DecodeParams& p, Place& at) {
   __shared__ unsigned part[kDecWarps];
   __shared__ uint4 shared_found[kDecWarps];
