@@ -347,9 +347,9 @@ RBS_API rbs_status rbs_paged_extend(const rbs_paged_shape* shape, const int* seq
 typedef struct {
   const int* positions;    /* device, n_tokens ints; any sign */
   const float* inv_freq;   /* device, rot_dim / 2 floats (NULL if rot_dim == 0) */
-  const float* q_norm;     /* device, 128 floats, or NULL */
-  const float* k_norm;     /* device, 128 floats, or NULL */
-  float eps;               /* >= 0 */
+  const float* q_norm;     /* device, 128 floats, 16-byte aligned, or NULL */
+  const float* k_norm;     /* device, 128 floats, 16-byte aligned, or NULL */
+  float eps;               /* >= 0; taken as at least the smallest normal number, 2^-126 */
   float magnitude;         /* finite */
   int rot_dim;             /* 0 .. 128, a multiple of 8 (RBS_ERR_UNSUPPORTED otherwise) */
   int interleaved;         /* 0 or 1 */

@@ -530,7 +530,7 @@ def rbs_qk_norm_rope(Q: torch.Tensor, K: torch.Tensor, positions: torch.Tensor, 
                      q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6,
                      interleaved: bool = False, magnitude: float = 1.0, out_q: torch.Tensor | None = None,
                      out_k: torch.Tensor | None = None):
-    """Norm of each head (weights q_norm, k_norm [128] fp32; None: no norm) and rotation by position of the first
+    """Norm of each head (weights q_norm, k_norm [128] fp32, 16-byte aligned; None: no norm) and rotation by position of the first
     2 * len(inv_freq) elements of every head, in one pass.  Q, K: [tokens, heads, 128] or [batch, tokens, heads, 128] bf16, any
     strides (slices of a fused projection); positions [tokens] int32, inv_freq fp32 (rope_frequencies; None: no rotation).
     interleaved: pairs are neighbours instead of halves apart.  out_q is Q, out_k is K: in place.  Returns (Q', K')."""

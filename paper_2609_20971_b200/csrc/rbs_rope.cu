@@ -1,7 +1,8 @@
 // rbs_qk_norm_rope and rbs_qk_norm_rope_paged: norm of each head and rotation by position in one pass over the rows of Q
 // and K (256 bytes each), in the paged form with the keys and the values going to their slots of the cache.
-// A stream: 512 bytes read and written per row against some 60 instructions of half a warp.  128K tokens of 32 + 4 heads: 367 us
-// = 6.6 TB/s, what a plain copy reaches.
+// A stream: 512 bytes read and written per row against some 50 instructions of half a warp.  128K tokens of 32 + 4 heads: 363 us
+// = 6.65 TB/s, a little above what a plain copy reaches.  Instructions count all the same: with a quarter more of them (offsets by
+// head, weights one by one, rsqrtf's care for denormals) 400 us.
 #include <type_traits>
 
 #include "rbs_common.cuh"
@@ -25,7 +26,7 @@ struct RopeParams {
   int rot, Hq, Hkv, N, page;
   int slot_rows, cache_rows;   // entries of slots; rows of the cache
   long long tokens;      // batch * N
-  int spread;            // warps per token: 1, 2, 4 or 8
+  int spread;            // log2 of the warps per token: 0 .. 3
 };
 
 constexpr int kRopeThreads = 256;
@@ -46,6 +47,13 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return d;
 }
 
+// of a normal number
+__device__ __forceinline__ float fast_rsqrt(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Half a warp per row.  Lane u (of 16) of a row holds two groups A, B of four elements:
 //   half layout, u < rot / 8: A = 4u.., B = rot/2 + 4u.., so that pair 4u + k is (A[k], B[k]);
 //   otherwise 8 neighbours: A = 8u.., B = 8u + 4..; interleaved, pairs 4u .. 4u + 3 are (A0,A1) (A2,A3) (B0,B1) (B2,B3).
@@ -56,19 +64,36 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
 template <bool INTERLEAVED, bool WHOLE>
 struct RopeLane {
   float2 c[4], s[4];   // element j of this lane becomes x_j c_j + x_(partner of j) s_j
-  int a, b;
+  int a, gap;          // A's first element, elements from there to B's: a constant where that helps
   float eps;
   bool turns;
 
+  __device__ __forceinline__ void place(int rot) {
+    const int u = threadIdx.x & 15;
+    turns = WHOLE || u < rot / 8;
+    a = turns && !INTERLEAVED ? 4 * u : 8 * u;
+    gap = turns && !INTERLEAVED ? rot / 2 : 4;
+  }
+  __device__ __forceinline__ int to_b() const { return INTERLEAVED ? 4 : WHOLE ? kHeadDim / 2 : gap; }
   __device__ __forceinline__ void weigh(const float2* angles, const float* weights) {
     const int u = threadIdx.x & 15;
     const bool norm = weights != nullptr;
     float w[8], cj[8], sj[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = norm ? weights[(j < 4 ? a : b - 4) + j] : 1.0f;
+    for (int j = 0; j < 8; ++j) w[j] = 1.0f;
+    if (norm) {
+      const float4 wa = *reinterpret_cast<const float4*>(weights + a), wb = *reinterpret_cast<const float4*>(weights + a + to_b());
+      w[0] = wa.x; w[1] = wa.y; w[2] = wa.z; w[3] = wa.w;
+      w[4] = wb.x; w[5] = wb.y; w[6] = wb.z; w[7] = wb.w;
+    }
+    float4 two[2] = {make_float4(1.f, 0.f, 1.f, 0.f), make_float4(1.f, 0.f, 1.f, 0.f)};
+    if (WHOLE || turns) {
+      two[0] = *reinterpret_cast<const float4*>(angles + 4 * u);
+      two[1] = *reinterpret_cast<const float4*>(angles + 4 * u + 2);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float2 cs = WHOLE || turns ? angles[4 * u + k] : make_float2(1.0f, 0.0f);
+      const float2 cs = k & 1 ? make_float2(two[k >> 1].z, two[k >> 1].w) : make_float2(two[k >> 1].x, two[k >> 1].y);
       const int f = INTERLEAVED ? 2 * k : k, g = INTERLEAVED ? 2 * k + 1 : 4 + k;
       cj[f] = w[f] * cs.x; sj[f] = -w[g] * cs.y;
       cj[g] = w[g] * cs.x; sj[g] = w[f] * cs.y;
@@ -106,7 +131,7 @@ struct RopeLane {
         for (int i = 0; i < N; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float r = rsqrtf(sum[i] * (1.0f / kHeadDim) + eps);
+        const float r = fast_rsqrt(sum[i] * (1.0f / kHeadDim) + eps);
 #pragma unroll
         for (int k = 0; k < 4; ++k) y[i][k] = mul2(y[i][k], make_float2(r, r));
       }
@@ -120,43 +145,46 @@ struct RopeLane {
 };
 
 // The rows of one warp, two heads at a time, in order: its heads of Q, of K, of V.  kRopeAhead groups of kRopeGroup such pairs are on
-// their way to a ring of its own in shared memory (in registers they would cost as many as the arithmetic; pair by pair a
-// chunk of 8,191 tokens of 64 heads takes 59.8 us instead of 57.7, 128K tokens of 32 heads 386 instead of 392).  All but the
-// second head of a last pair is the same for both halves, so that the warp stays together: halves that went through loops of their own took twice the
-// instructions (447 us instead of 367 for 128K tokens of 36 heads).
+// their way to a ring of its own in shared memory (in registers they would cost as many as the arithmetic; a chunk of 8,191 tokens
+// of 64 heads takes 59.8 us pair by pair, 57.7 with two pairs).  All but the second head of a last pair is the same for both
+// halves, so that the warp stays together: halves that went through loops of their own took twice the instructions (447 us instead
+// of 367 for 128K tokens of 36 heads).
 struct RopeRows {
   const __nv_bfloat16* at;       // this half's row that is fetched next, at this lane's 16 bytes
   int64_t skip;                  // elements from it to the one behind it
-  int kind, left;                // its kind, pairs of that kind that are left
-  int head, heads, step;         // its head, of how many, heads to the one behind it
-  uint32_t ring, fill, read;     // shared memory: this half's first slot, and the byte offsets of the slots filled and read next
+  int kind, left, mine;          // its kind; pairs of that kind that are left, and rows of this half
+  uint32_t fill, read;           // shared memory: the group filled next at this lane's 16 bytes, and the one read next at its A;
+  int hop;                       // from it to the ring's other one
 
   template <typename Open>
   __device__ __forceinline__ void fetch(Open& open) {
     if (left <= 0 && kind < 2) open(*this, kind + 1);
 #pragma unroll
     for (int j = 0; j < kRopeGroup; ++j) {
-      if (j < left && head < heads) cp_async16_zfill(ring + fill + j * 512 + (threadIdx.x & 15) * 16, at, true);
+      if (j < mine) cp_async16_zfill(fill + j * 512, at, true);
       at += skip;
-      head += step;
     }
     left -= kRopeGroup;
+    mine -= kRopeGroup;
     cp_async_commit();
-    fill = fill == (kRopeAhead - 1) * kRopeGroup * 512 ? 0 : fill + kRopeGroup * 512;
+    fill += hop;
+    read += hop;
+    hop = -hop;
   }
-  // the next group has arrived: the address of this half's row of its first pair
+  // the next group has arrived: the address of A of this half's row of its first pair
   __device__ __forceinline__ uint32_t wait() {
     cp_async_wait<kRopeAhead - 1>();
     __syncwarp();
-    return ring + read;
+    return read;
   }
   template <typename Open>
   __device__ __forceinline__ void done(Open& open) {
     __syncwarp();
-    read = read == (kRopeAhead - 1) * kRopeGroup * 512 ? 0 : read + kRopeGroup * 512;
     fetch(open);
   }
 };
+// Both are filled before the first is read, and each is filled again as soon as it is read: the group to fill is the one to read.
+static_assert(kRopeAhead == 2, "two groups take turns");
 __device__ __forceinline__ uint2 lds64(uint32_t at) {
   uint2 v;
   asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
@@ -168,20 +196,18 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   return v;
 }
 
-// A CTA has 8 / spread tokens, `spread` warps for each.  Its threads compute the tokens' angles once, behind the first rows'
+// A CTA has eight warps, 2^spread for each of its tokens.  Its threads compute the tokens' angles once, behind the first rows'
 // loads.
 template <bool INTERLEAVED, bool WHOLE, bool PAGED>
 __global__ void __launch_bounds__(kRopeThreads, kRopeResident)
 rope_kernel(const RopeParams p) {
-  __shared__ float2 angles[kRopeWarps][kHeadDim / 2];
+  __shared__ __align__(16) float2 angles[kRopeWarps][kHeadDim / 2];
   __shared__ __align__(16) unsigned char rings[kRopeWarps * kRopeAhead * kRopeGroup * 512];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), u = threadIdx.x & 15, side = (threadIdx.x >> 4) & 1;
-  const int per_cta = kRopeWarps / p.spread, mine = warp / p.spread, pair0 = warp - mine * p.spread, h0 = 2 * pair0 + side;
+  const int per_cta = kRopeWarps >> p.spread, mine = warp >> p.spread, pair0 = warp - (mine << p.spread), h0 = 2 * pair0 + side;
   const long long token0 = static_cast<long long>(blockIdx.x) * per_cta, token = token0 + mine;
   RopeLane<INTERLEAVED, WHOLE> lane;
-  lane.turns = WHOLE || u < p.rot / 8;
-  lane.a = lane.turns && !INTERLEAVED ? 4 * u : 8 * u;
-  lane.b = lane.turns && !INTERLEAVED ? p.rot / 2 + 4 * u : 8 * u + 4;
+  lane.place(p.rot);
   lane.eps = p.eps;
   pdl_trigger();
   pdl_wait();
@@ -193,7 +219,7 @@ rope_kernel(const RopeParams p) {
   const bool angle = k < p.rot / 2 && first < per_cta && token0 + first < p.tokens;
   const float freq = angle ? p.inv_freq[k] : 0.f;
   int pos = angle ? position(first) : 0;
-  if (p.spread > 1 && threadIdx.x < 2 * kHeadDim * 4 / 128) {
+  if (p.spread > 0 && threadIdx.x < 2 * kHeadDim * 4 / 128) {
     const float* w = threadIdx.x & 1 ? p.k_norm : p.q_norm;
     if (w != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(w + (threadIdx.x >> 1) * 32));
   }
@@ -209,11 +235,12 @@ rope_kernel(const RopeParams p) {
     }
   }
   // pairs of heads of this warp
-  auto pairs = [&](int heads) { return (((heads + 1) >> 1) - pair0 + p.spread - 1) / p.spread; };
+  auto pairs = [&](int heads) { return (((heads + 1) >> 1) - pair0 + (1 << p.spread) - 1) >> p.spread; };
   const int n_q = live ? pairs(p.Hq) : 0;
   const int n_k = live && (!PAGED || kc != nullptr || p.Ko != nullptr) ? pairs(p.Hkv) : 0;
   const int n_v = PAGED && vc != nullptr ? n_k : 0;
-  const int step = 2 * p.spread;
+  const int step = 2 << p.spread;
+  auto rows_of = [&](int heads) { return (heads - h0 + step - 1) >> (p.spread + 1); };      // of this half
   auto open = [&](RopeRows& r, int kind) {      // the first row of that kind, or of the next one that there is
     if (kind == 0 && n_q == 0) kind = 1;
     const bool q = kind == 0, k = kind == 1;
@@ -223,14 +250,13 @@ rope_kernel(const RopeParams p) {
     r.skip = step * stride;
     r.left = q ? n_q : k ? n_k : kind == 2 ? n_v : 0;
     r.kind = kind;
-    r.head = h0;
-    r.heads = q ? p.Hq : p.Hkv;
+    r.mine = min(r.left, rows_of(q ? p.Hq : p.Hkv));
   };
   RopeRows rows;
-  rows.step = step;
-  rows.left = 0;
-  rows.ring = smem_u32(rings) + warp * kRopeAhead * kRopeGroup * 512 + side * 256;
-  rows.fill = rows.read = 0;
+  rows.left = rows.mine = 0;
+  rows.fill = smem_u32(rings) + warp * kRopeAhead * kRopeGroup * 512 + side * 256 + u * 16;
+  rows.read = rows.fill - u * 16 + lane.a * 2;
+  rows.hop = kRopeGroup * 512;
   open(rows, 0);
 #pragma unroll
   for (int i = 0; i < kRopeAhead; ++i) rows.fetch(open);
@@ -254,57 +280,58 @@ rope_kernel(const RopeParams p) {
   __syncthreads();
   if (!live) return;
 
-  const uint32_t at_a = lane.a * 2, at_b = lane.b * 2;
-  auto put = [&](__nv_bfloat16* row, const uint2& xa, const uint2& xb) {
-    *reinterpret_cast<uint2*>(row + lane.a) = xa;
-    *reinterpret_cast<uint2*>(row + lane.b) = xb;
-  };
-  auto turn_rows = [&](auto norm, int n, int heads, __nv_bfloat16* dst, int64_t skip, __nv_bfloat16* dst2, int64_t skip2) {
-    for (int i = 0, h = h0; i < n; i += kRopeGroup) {
+  // rows of `dst` (and of `dst2`) at this lane's A
+  auto turn_rows = [&](auto norm, int n, int mine, __nv_bfloat16* dst, int64_t skip, __nv_bfloat16* dst2, int64_t skip2) {
+    auto put = [&](__nv_bfloat16* at, const uint2& xa, const uint2& xb) {
+      *reinterpret_cast<uint2*>(at) = xa;
+      *reinterpret_cast<uint2*>(at + lane.to_b()) = xb;
+    };
+    for (; n > 0; n -= kRopeGroup, mine -= kRopeGroup) {
       const uint32_t from = rows.wait();
       uint2 xa[kRopeGroup], xb[kRopeGroup];
 #pragma unroll
-      for (int j = 0; j < kRopeGroup; ++j) {      // a pair that is not there is turned and not written
-        xa[j] = lds64(from + j * 512 + at_a);
-        xb[j] = lds64(from + j * 512 + at_b);
+      for (int j = 0; j < kRopeGroup; ++j) {      // a row that is not there is turned and not written
+        xa[j] = lds64(from + j * 512);
+        xb[j] = lds64(from + j * 512 + lane.to_b() * 2);
       }
       rows.done(open);
       lane.template turn<decltype(norm)::value>(xa, xb);
 #pragma unroll
       for (int j = 0; j < kRopeGroup; ++j) {
-        if (i + j < n && h < heads) {
+        if (j < mine) {
           if (!PAGED || dst != nullptr) put(dst, xa[j], xb[j]);
           if (PAGED && dst2 != nullptr) put(dst2, xa[j], xb[j]);
         }
         if (!PAGED || dst != nullptr) dst += skip;
         if (PAGED && dst2 != nullptr) dst2 += skip2;
-        h += step;
       }
     }
   };
   if (n_q > 0) {
     lane.weigh(angles[mine], p.q_norm);
-    __nv_bfloat16* out = p.Qo + l * p.qosb + t * p.qost + h0 * p.qosh;
-    if (p.q_norm != nullptr) turn_rows(std::true_type(), n_q, p.Hq, out, step * p.qosh, nullptr, 0);
-    else turn_rows(std::false_type(), n_q, p.Hq, out, step * p.qosh, nullptr, 0);
+    __nv_bfloat16* out = p.Qo + l * p.qosb + t * p.qost + h0 * p.qosh + lane.a;
+    if (p.q_norm != nullptr) turn_rows(std::true_type(), n_q, rows_of(p.Hq), out, step * p.qosh, nullptr, 0);
+    else turn_rows(std::false_type(), n_q, rows_of(p.Hq), out, step * p.qosh, nullptr, 0);
   }
   if (n_k > 0) {
     lane.weigh(angles[mine], p.k_norm);
-    __nv_bfloat16* out = PAGED && p.Ko == nullptr ? nullptr : p.Ko + l * p.kosb + t * p.kost + h0 * p.kosh;
-    __nv_bfloat16* out2 = PAGED && kc != nullptr ? kc + h0 * p.kch : nullptr;
-    if (p.k_norm != nullptr) turn_rows(std::true_type(), n_k, p.Hkv, out, step * p.kosh, out2, step * p.kch);
-    else turn_rows(std::false_type(), n_k, p.Hkv, out, step * p.kosh, out2, step * p.kch);
+    __nv_bfloat16* out = PAGED && p.Ko == nullptr ? nullptr : p.Ko + l * p.kosb + t * p.kost + h0 * p.kosh + lane.a;
+    __nv_bfloat16* out2 = PAGED && kc != nullptr ? kc + h0 * p.kch + lane.a : nullptr;
+    if (p.k_norm != nullptr) turn_rows(std::true_type(), n_k, rows_of(p.Hkv), out, step * p.kosh, out2, step * p.kch);
+    else turn_rows(std::false_type(), n_k, rows_of(p.Hkv), out, step * p.kosh, out2, step * p.kch);
   }
   if (PAGED) {
-    for (int i = 0, h = h0; i < n_v; i += kRopeGroup) {
-      const uint32_t from = rows.wait() + u * 16;
+    __nv_bfloat16* dst = vc + h0 * p.vch + 8 * u;
+    int mine = rows_of(p.Hkv);
+    for (int n = n_v; n > 0; n -= kRopeGroup, mine -= kRopeGroup) {
+      const uint32_t from = rows.wait() - lane.a * 2 + u * 16;
       uint4 x[kRopeGroup];
 #pragma unroll
       for (int j = 0; j < kRopeGroup; ++j) x[j] = lds128(from + j * 512);
       rows.done(open);
 #pragma unroll
-      for (int j = 0; j < kRopeGroup; ++j, h += step)
-        if (i + j < n_v && h < p.Hkv) *reinterpret_cast<uint4*>(vc + h * p.vch + 8 * u) = x[j];
+      for (int j = 0; j < kRopeGroup; ++j, dst += step * p.vch)
+        if (j < mine) *reinterpret_cast<uint4*>(dst) = x[j];
     }
   }
 }
@@ -315,13 +342,13 @@ static rbs_status check_rope(const rbs_rope* r, int n_tokens) {
   if (r->rot_dim < 0 || (r->interleaved != 0 && r->interleaved != 1)) return RBS_ERR_INVALID_ARG;
   if (r->rot_dim > kHeadDim || r->rot_dim % 8 != 0) return RBS_ERR_UNSUPPORTED;
   if (r->rot_dim > 0 && r->inv_freq == nullptr) return RBS_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(r->q_norm) % 4 != 0 || reinterpret_cast<uintptr_t>(r->k_norm) % 4 != 0) return RBS_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(r->q_norm) % 16 != 0 || reinterpret_cast<uintptr_t>(r->k_norm) % 16 != 0) return RBS_ERR_INVALID_ARG;
   return RBS_OK;
 }
 
 static void set_rope(RopeParams& p, const rbs_rope* r) {
   p.positions = r->positions; p.inv_freq = r->inv_freq; p.q_norm = r->q_norm; p.k_norm = r->k_norm;
-  p.eps = r->eps; p.magnitude = r->magnitude; p.rot = r->rot_dim;
+  p.eps = fmaxf(r->eps, 1.17549435e-38f); p.magnitude = r->magnitude; p.rot = r->rot_dim;
 }
 
 // A token is spread over as many of 8, 4, 2 warps as leave all CTAs resident at a time, and stays with one warp where that does not
@@ -331,8 +358,8 @@ static void set_rope(RopeParams& p, const rbs_rope* r) {
 static rbs_status launch_rope(RopeParams p, long long tokens, bool interleaved, bool paged, cudaStream_t s) {
   const long long room = static_cast<long long>(kRopeResident) * sm_count() * kRopeWarps;
   const bool many = p.Hq + p.Hkv * (paged ? 2 : 1) >= 64;
-  p.spread = tokens * 8 <= room ? 8 : tokens * 4 <= room ? 4 : tokens * 2 <= (many ? 4 : 1) * room ? 2 : 1;
-  const long long per_cta = kRopeWarps / p.spread, ctas = (tokens + per_cta - 1) / per_cta;
+  p.spread = tokens * 8 <= room ? 3 : tokens * 4 <= room ? 2 : tokens * 2 <= (many ? 4 : 1) * room ? 1 : 0;
+  const long long per_cta = kRopeWarps >> p.spread, ctas = (tokens + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffffll) return RBS_ERR_UNSUPPORTED;
   p.tokens = tokens;
   using Kernel = void (*)(const RopeParams);

@@ -107,7 +107,8 @@ def _check_turn(got, x, positions, freq, weight, **more):
     assert (err <= STEP * np.abs(want) + 32 * 2.0 ** -24 * size).all(), float((err / (np.abs(want) + 1e-30)).max())
 
 
-@pytest.mark.parametrize("tokens, hq, hkv", [(1, 1, 1), (1, 32, 4), (3, 3, 1), (61, 40, 8), (257, 16, 16), (1003, 8, 2)])
+# of the many tokens each with another number of warps to a token, and a last thread block with fewer tokens than the others
+@pytest.mark.parametrize("tokens, hq, hkv", [(1, 1, 1), (1, 32, 4), (3, 3, 1), (61, 40, 8), (257, 16, 16), (1003, 8, 2), (1501, 5, 1), (5003, 3, 2)])
 @pytest.mark.parametrize("rot, interleaved, norm", [(128, False, True), (128, True, True), (64, False, False), (64, True, True), (96, False, True),
                                                     (8, True, False), (8, False, True), (0, False, True)])
 def test_norm_rope_equals_the_oracle(tokens, hq, hkv, rot, interleaved, norm):
@@ -147,6 +148,17 @@ def test_angles_of_far_positions_are_exact():
     assert (np.abs(_f64(oq) - want) <= STEP * np.abs(want) + 40 * 2.0 ** -24 * size).all()
 
 
+def test_norm_of_zeros_and_of_small_and_large_rows():
+    q = _randn(7, 6, 2, 128)
+    for row, scale in enumerate((0.0, 1e-12, 1e-18, 1e12, 3e17)):
+        q[row] *= scale
+    pos, w = torch.arange(6, dtype=torch.int32, device="cuda"), torch.rand(128, device="cuda") + 0.5
+    for eps in (1e-6, 0.0):
+        oq, _ = rbs_qk_norm_rope(q, q, pos, _frequencies(128), q_norm=w, k_norm=w, eps=eps)
+        # the smallest normal number in place of a zero eps: the mean square of the smallest row here is 1e-36
+        _check_turn(oq, q, pos, _frequencies(128), w, eps=max(eps, 2.0 ** -126))
+
+
 def test_norm_rope_keeps_nan_and_infinity_in_their_rows():
     q = _randn(6, 5, 3, 128)
     q[1, 2, 7], q[3, 0, 100] = float("nan"), float("inf")
@@ -166,7 +178,7 @@ def _cache(seed, pages, page, hkv, order):
 
 
 @pytest.mark.parametrize("tokens, hq, hkv, page, order", [(1, 32, 4, 64, "token"), (48, 32, 4, 16, "head"), (3, 3, 1, 1, "token"), (129, 40, 8, 24, "token"),
-                                                          (700, 16, 16, 256, "head")])
+                                                          (700, 16, 16, 256, "head"), (1501, 6, 3, 64, "token"), (5003, 8, 2, 16, "head")])
 @pytest.mark.parametrize("keep_k", [False, True])
 def test_norm_rope_paged_writes_its_slots_and_nothing_else(tokens, hq, hkv, page, order, keep_k):
     pages = tokens // page + 3

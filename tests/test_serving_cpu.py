@@ -67,7 +67,7 @@ def _turn(**change):
     return RbsRope(**v)
 
 
-BAD_TURNS = [(dict(positions=None), INVALID), (dict(inv_freq=None), INVALID), (dict(q_norm=P + 2), INVALID), (dict(k_norm=P + 1), INVALID),
+BAD_TURNS = [(dict(positions=None), INVALID), (dict(inv_freq=None), INVALID), (dict(q_norm=P + 4), INVALID), (dict(k_norm=P + 8), INVALID),
              (dict(eps=-1.0), INVALID), (dict(eps=NAN), INVALID), (dict(eps=INF), INVALID), (dict(magnitude=NAN), INVALID),
              (dict(magnitude=INF), INVALID), (dict(rot_dim=-8), INVALID), (dict(interleaved=2), INVALID), (dict(rot_dim=136), UNSUPPORTED),
              (dict(rot_dim=20), UNSUPPORTED)]
