@@ -1,7 +1,7 @@
 // rbs_qk_norm_rope and rbs_qk_norm_rope_paged: norm of each head and rotation by position in one pass over the rows of Q
 // and K (256 bytes each), in the paged form with the keys and the values going to their slots of the cache.
-// A stream: 512 bytes read and written per row against some 50 instructions of half a warp.  128K tokens of 32 + 4 heads: 363 us
-// = 6.65 TB/s, a little above what a plain copy reaches.  Instructions count all the same: with a quarter more of them (offsets by
+// A stream: 512 bytes read and written per row against some 50 instructions of half a warp.  128K tokens of 32 + 4 heads: 364 us
+// = 6.64 TB/s, a little above what a plain copy reaches.  Instructions count all the same: with a quarter more of them (offsets by
 // head, weights one by one, rsqrtf's care for denormals) 400 us.
 #include <type_traits>
 
@@ -353,8 +353,8 @@ static void set_rope(RopeParams& p, const rbs_rope* r) {
 
 // A token is spread over as many of 8, 4, 2 warps as leave all CTAs resident at a time, and stays with one warp where that does not
 // fit: a spread shortens the row of pairs that a warp goes through, and costs the weights of each warp.  us with 1 / 2 / 4 / 8 warps,
-// 36 heads: 400 tokens 6.6 / 5.5 / 5.2 / 4.8; 1,003 8.9 / 8.4 / 6.9 / 9.1; 2,000 11.9 / 10.0 / 12.0 / 14.9; 4,000 15.5 / 17.1 / 20.0 / 27.1.
-// Where a token has many rows two warps go on paying for four times as many (80 rows: 4,000 tokens 33.3 / 30.6, 8,000 56.7 / 55.7).
+// 36 heads: 400 tokens 6.2 / 4.9 / 4.5 / 4.3; 1,003 7.9 / 7.3 / 6.3 / 7.7; 2,000 10.6 / 9.2 / 10.2 / 12.3; 3,000 12.2 / 13.1 / 13.6 / 16.8.
+// Where a token has many rows two warps go on paying for four times as many (80 rows: 4,000 tokens 32.3 / 29.7, 8,000 56.3 / 55.4).
 static rbs_status launch_rope(RopeParams p, long long tokens, bool interleaved, bool paged, cudaStream_t s) {
   const long long room = static_cast<long long>(kRopeResident) * sm_count() * kRopeWarps;
   const bool many = p.Hq + p.Hkv * (paged ? 2 : 1) >= 64;
