@@ -93,25 +93,27 @@ struct Softmax {
     }
   }
 
-  // Scores of 16 keys; `valid`: a bit per key.  p: their probabilities against the maximum in use, as the B operands of P V: each
-  // is split into two bf16 numbers, off by 2^-17 relative, so that the output sees no rounding but its own (error against
-  // 64 bits 1.7e-3 instead of 2.3e-3, for 0.3 - 0.8 % of the time).
+  // Scores of 16 keys and, in c, their probabilities against the maximum in use; `valid`: a bit per key.
   // The maximum moves only when a score passes it by kDecSlack: probabilities of up to 2^8 round no worse, and a tile that
   // leaves it alone has no exchange between lanes and no rescaling.
-  __device__ __forceinline__ void scores(const Queries<HT>& q, uint32_t ktile, uint32_t valid, float scale_log2, uint32_t (&p)[HT][4]) {
+  __device__ __forceinline__ void scores(const Queries<HT>& q, uint32_t ktile, uint32_t valid, float scale_log2, float (&c)[HT][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2;
-    float c[HT][4];
+    float c2[HT][4];
 #pragma unroll
     for (int n = 0; n < HT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) c[n][i] = 0.f;
+      for (int i = 0; i < 4; ++i) c[n][i] = c2[n][i] = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 8; ++k) {      // two sums of four steps: half as many roundings in a row
       uint32_t a[4];
       ldmatrix_x4(a[0], a[1], a[2], a[3], ktile + tile_off(lane & 15, 2 * k + (lane >> 4)));
 #pragma unroll
-      for (int n = 0; n < HT; ++n) mma_bf16_16816(c[n], a, q.q[n][2 * k], q.q[n][2 * k + 1]);
+      for (int n = 0; n < HT; ++n) mma_bf16_16816(k & 1 ? c2[n] : c[n], a, q.q[n][2 * k], q.q[n][2 * k + 1]);
     }
+#pragma unroll
+    for (int n = 0; n < HT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[n][i] += c2[n][i];
     const bool lo = (valid >> g) & 1, hi = (valid >> (g + 8)) & 1;
     bool move = false;
 #pragma unroll
@@ -150,25 +152,42 @@ struct Softmax {
         c[n][i + 2] = fast_exp2(c[n][i + 2] - base);
         l[n][i] += c[n][i] + c[n][i + 2];
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t high = pack_bf16(c[n][2 * i], c[n][2 * i + 1]);
-        p[n][i] = transpose_8x8(high);
-        p[n][i + 2] = transpose_8x8(pack_bf16(c[n][2 * i] - bf16lo(high), c[n][2 * i + 1] - bf16hi(high)));
-      }
     }
   }
 
-  __device__ __forceinline__ void values(uint32_t vtile, const uint32_t (&p)[HT][4]) {
+  // Adds P V of 16 keys.  A probability goes into the product as three bf16 numbers, which together are the fp32 number, off by 2^-25
+  // of it.  The sums of the product drop bits where a plain addition rounds, and over the hundred tiles of a share those would add
+  // up in one direction: a tile is summed from zero, the smallest parts first, and added by itself.  Against 64 bits rounded to bf16,
+  // 2-norm, 64 sequences of 64 heads: two bf16 numbers and one running sum 1.2e-4 (207.9 us), three numbers the same (210.2),
+  // with tiles summed by themselves 3.9e-5 (212.7), with the scores' product in two sums as well 2.9e-5 (212.9); plain fp32
+  // operations 5.8e-5.
+  __device__ __forceinline__ void values(uint32_t vtile, const float (&c)[HT][4]) {
     const int lane = threadIdx.x & 31;
+    uint32_t p[HT][6];
+#pragma unroll
+    for (int n = 0; n < HT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float x = c[n][2 * i], y = c[n][2 * i + 1];
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          const uint32_t rounded = pack_bf16(x, y);
+          p[n][2 * part + i] = transpose_8x8(rounded);
+          x -= bf16lo(rounded);
+          y -= bf16hi(rounded);
+        }
+      }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       uint32_t a[4];
       ldmatrix_x4_trans(a[0], a[1], a[2], a[3], vtile + tile_off((lane & 7) + (lane >> 4) * 8, 2 * j + ((lane >> 3) & 1)));
 #pragma unroll
       for (int n = 0; n < HT; ++n) {
-        mma_bf16_16816(o[n][j], a, p[n][0], p[n][1]);
-        mma_bf16_16816(o[n][j], a, p[n][2], p[n][3]);
+        float sum[4] = {};
+#pragma unroll
+        for (int part = 4; part >= 0; part -= 2) mma_bf16_16816(sum, a, p[n][part], p[n][part + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][j][i] += sum[i];
       }
     }
   }
@@ -661,7 +680,7 @@ decode_kernel(const DecodeParams p) {
       const uint32_t kt = ring + 2 * (i % kDecStages) * kDecTileBytes, vt = kt + kDecTileBytes;
       const uint32_t word = queue[0];
       queue[0] = queue[1];
-      uint32_t pr[HT][4];
+      float pr[HT][4];
       cp_async_wait<2 * kDecStages - 1>();
       __syncwarp();
       sm.scores(q, kt, word & 0xffffu, p.scale_log2, pr);

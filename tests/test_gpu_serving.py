@@ -344,6 +344,32 @@ def test_decode_of_one_dominant_key_and_of_scores_far_apart():
     assert np.abs(_f64(lse) - l).max() <= 1e-3
 
 
+@pytest.mark.parametrize("hq, hkv", [(8, 8), (16, 1)])
+def test_decode_keeps_probabilities_in_32_bits(hq, hkv):
+    """Values that cancel: two keys of score 0 hold the negative of what the third key's probability makes of its value, to 2^-17 of
+    it, so that the output's own rounding leaves the probability's in sight.
+    The score is one product, |x| <= 2 in log2 units: its scale is rounded three times, 3 * 2^-24 |x|, and the exponential is off by 2^-22:
+    together below 2^-21 of a probability that makes up half of `size`.  Three terms in fp32 with up to three products each leave
+    9 * 2^-24 of it, so 2^-20 covers all.  Two bf16 numbers in place of a probability are off by up to 2^-18."""
+    g = np.random.default_rng(5)
+    seqs = 64
+    bf16 = lambda x: torch.tensor(x).to(torch.bfloat16).double().numpy()  # noqa: E731
+    x, w = bf16(g.uniform(0.25, 15.0, (seqs, hkv))), bf16(g.uniform(1.0, 2.0, (seqs, hkv, 128)))
+    want = -np.exp(-x / np.sqrt(128.0))[..., None] * w
+    q = np.zeros((seqs, hkv, hq // hkv, 128))
+    q[..., 0] = x[..., None]
+    k, v = np.zeros((seqs, 16, hkv, 128)), np.zeros((seqs, 16, hkv, 128))
+    k[:, 2, :, 0], v[:, 2] = -1.0, w
+    v[:, 0] = bf16(want)
+    v[:, 1] = bf16(want - v[:, 0])
+    q, k, v = (torch.tensor(t, device="cuda").to(torch.bfloat16) for t in (q.reshape(seqs, hq, 128), k, v))
+    table, lens = torch.arange(seqs, dtype=torch.int32, device="cuda")[:, None], _ints([3] * seqs)
+    out = rbs_paged_decode(q, k, v, table, lens)
+    ref, _, size = so.decode(_f64(q), _f64(k), _f64(v), table.cpu().numpy(), lens.cpu().numpy())
+    assert np.abs(ref).max() < 2.0 ** -16 * size.max()
+    assert (np.abs(_f64(out) - ref) <= STEP * np.abs(ref) + 2.0 ** -20 * size).all()
+
+
 def test_decode_passes_nan_of_a_key_on_to_the_heads_that_read_it():
     k, v, table, lens = _sequences(15, [100, 100], 16, 2)
     q = _randn(16, 2, 8, 128)
