@@ -53,6 +53,12 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+// A bf16 number below x > 0, by 2^-9 to 2^-6 of x, as fp32 bits; 0 for 0, NaN for NaN.  What is left of x in two steps has at most 10
+// bits and is positive.  (Below some 2^-110 the last part is lost: an infinite value with a weight that small gives NaN, as it does
+// where the weight itself underflows.)
+__device__ __forceinline__ uint32_t bf16_below(float x) {
+  return static_cast<uint32_t>(max(__float_as_int(x) - 0x8000, 0)) & 0xffff0000u;
+}
 // The value that exponentials are taken against: nothing seen yet must not give inf - inf.
 __device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (exp_base(m) + log2f(l)) * 0.6931471805599453f; }
@@ -155,8 +161,8 @@ struct Softmax {
     }
   }
 
-  // Adds P V of 16 keys.  A probability goes into the product as three bf16 numbers, which together are the fp32 number, off by 2^-25
-  // of it.  The sums of the product drop bits where a plain addition rounds, and over the hundred tiles of a share those would add
+  // Adds P V of 16 keys.  A probability goes into the product as three bf16 numbers, which together are the fp32 number, off by 2^-24
+  // of it, and none of which is zero or below: an infinite value stays what it is in each of the three products.  The sums of the product drop bits where a plain addition rounds, and over the hundred tiles of a share those would add
   // up in one direction: a tile is summed from zero, the smallest parts first, and added by itself.  Against 64 bits rounded to bf16,
   // 2-norm, 64 sequences of 64 heads: two bf16 numbers and one running sum 1.2e-4 (207.9 us), three numbers the same (210.2),
   // with tiles summed by themselves 3.9e-5 (212.7), with the scores' product in two sums as well 2.9e-5 (212.9); plain fp32
@@ -170,12 +176,13 @@ struct Softmax {
       for (int i = 0; i < 2; ++i) {
         float x = c[n][2 * i], y = c[n][2 * i + 1];
 #pragma unroll
-        for (int part = 0; part < 3; ++part) {
-          const uint32_t rounded = pack_bf16(x, y);
-          p[n][2 * part + i] = transpose_8x8(rounded);
-          x -= bf16lo(rounded);
-          y -= bf16hi(rounded);
+        for (int part = 0; part < 2; ++part) {
+          const uint32_t px = bf16_below(x), py = bf16_below(y);
+          p[n][2 * part + i] = transpose_8x8(__byte_perm(px, py, 0x7632));
+          x -= __uint_as_float(px);
+          y -= __uint_as_float(py);
         }
+        p[n][4 + i] = transpose_8x8(pack_bf16(x, y));
       }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {

@@ -370,6 +370,31 @@ def test_decode_keeps_probabilities_in_32_bits(hq, hkv):
     assert (np.abs(_f64(out) - ref) <= STEP * np.abs(ref) + 2.0 ** -20 * size).all()
 
 
+@pytest.mark.parametrize("hq, page", [(8, 16), (8, 24), (32, 16)])
+def test_decode_passes_infinite_values_on(hq, page):
+    """Values of infinity, in keys of any weight: alone in its sequence, the maximum, somewhere in a sequence that many warps share."""
+    where = [(0, 0), (1, 0), (1, 1), (1, 2), (2, 50), (3, 0), (3, 2999), (3, 5999)]
+    k, v, table, lens = _sequences(17, [1, 3, 100, 6000], page, 2)
+    q = _randn(18, 4, hq, 128)
+    clean = rbs_paged_decode(q, k, v, table, lens)
+    inf, half = float("inf"), hq // 2      # heads of the second KV head
+    for s, t in where + [(2, None)]:       # None: in the key of largest weight of the first of those heads
+        if t is None:
+            t = np.argmax(_f64(k)[table[s, :-(-100 // page)].long().cpu().numpy(), :, 1].reshape(-1, 128)[:100] @ _f64(q)[s, half])
+        at = (int(table[s, int(t) // page]), int(t) % page, 1)
+        other = (int(table[s, 0]), 0, 1)
+        kept, kept_other = v[at].clone(), v[other].clone()
+        v[at][60], v[at][61], v[at][62] = inf, -inf, inf
+        if at != other:
+            v[other][62] = -inf            # the sum of both is no number
+        out = rbs_paged_decode(q, k, v, table, lens)
+        v[other], v[at] = kept_other, kept
+        assert bool((out[s, half:, 60] == inf).all() and (out[s, half:, 61] == -inf).all()), (s, t)
+        assert bool((out[s, half:, 62] == inf).all() if at == other else out[s, half:, 62].isnan().all())
+        out[s, half:, 60:63] = clean[s, half:, 60:63]
+        assert torch.equal(out, clean)
+
+
 def test_decode_passes_nan_of_a_key_on_to_the_heads_that_read_it():
     k, v, table, lens = _sequences(15, [100, 100], 16, 2)
     q = _randn(16, 2, 8, 128)
