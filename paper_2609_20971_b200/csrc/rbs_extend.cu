@@ -30,7 +30,8 @@ struct ExtendParams {
   unsigned int* status;   // of the debug build's checks
 };
 
-__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+// of a >= 0, without passing 31 bits for lengths and page sizes that come near them
+__device__ __forceinline__ int ceil_div(int a, int b) { return a / b + (a % b != 0); }
 
 struct TokensPages {
   long long tokens;
@@ -145,7 +146,7 @@ extend_kernel(const ExtendParams p) {
   const int fresh = total.pages, n_new = static_cast<int>(total.tokens);
   auto free_page = [&](int k) {      // page k of those that are taken
     const long long f = static_cast<long long>(used) + k;
-    return f < p.n_free ? p.free_pages[f] : -1;
+    return f >= 0 && f < p.n_free ? p.free_pages[f] : -1;
   };
   if (me == 0) p.free_used_out[0] = static_cast<int>(min(static_cast<long long>(used) + fresh, 0x7fffffffll));
   for (int s = me; s <= p.S; s += step) {

@@ -80,6 +80,27 @@ def test_extend_equals_the_oracle(seed, seqs, page, most, old, new, n_free, n_pa
     assert bool((whole[:, most:] == 77).all())
 
 
+@pytest.mark.parametrize("lens, add, page, most", [
+    ([2147482640, 0], [10, 1], 1000, 2147483),                            # a length within a page of 2^31
+    ([1000000000, 0, 1499999998], [5, 3, 4], 1500000000, 1),              # pages of more than 2^30 tokens
+    ([(1 << 30) + 3, 1 << 30, 0, 5], [4, 1, 0, 2], (1 << 30) + 1, 1)])
+def test_extend_of_lengths_and_page_sizes_near_31_bits(lens, add, page, most):
+    tokens, n_pages = sum(add) + 2, 0x7fffffff // page
+    table = np.full((len(lens), most), -1)
+    for s, n in enumerate(lens):
+        table[s, :-(-n // page)] = n_pages - 1
+    free = [0] * 3
+    want = so.extend(lens, add, table, free, page, n_pages, tokens)
+    whole = torch.full((3 * len(lens), most), 77, dtype=torch.int32, device="cuda")      # the table, and as much in front of it and behind
+    rows = whole[len(lens):2 * len(lens)]
+    rows.copy_(_ints(table))
+    out = rbs_paged_extend(_ints(lens), _ints(add), rows, _ints(free), page, n_pages, tokens)
+    for x, y in zip((rows, out.lens, out.cu, out.positions, out.slots), want):
+        assert np.array_equal(x.cpu().numpy(), y)
+    assert out.used.item() == want[5]
+    assert bool((whole[:len(lens)] == 77).all() and (whole[2 * len(lens):] == 77).all())
+
+
 def test_extend_step_after_step_hands_out_every_page_once():
     page, n_pages, seqs = 16, 61, 6
     g = np.random.default_rng(3)
