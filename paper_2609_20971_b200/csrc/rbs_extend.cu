@@ -204,7 +204,7 @@ extend_kernel(const ExtendParams p) {
         }
         if (good && pos[i] < cap) slot[i] = page * p.P + off;
       }
-      if (ROWS == 4 && p.aligned && row0 + ROWS <= p.T) {
+      if (ROWS == 4 && p.aligned && row0 <= p.T - ROWS) {      // row0 + ROWS may pass 31 bits
         *reinterpret_cast<int4*>(p.positions + row0) = make_int4(pos[0], pos[1 % ROWS], pos[2 % ROWS], pos[3 % ROWS]);
         *reinterpret_cast<int4*>(p.slots + row0) = make_int4(slot[0], slot[1 % ROWS], slot[2 % ROWS], slot[3 % ROWS]);
       } else {

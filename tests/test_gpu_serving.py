@@ -101,6 +101,20 @@ def test_extend_of_lengths_and_page_sizes_near_31_bits(lens, add, page, most):
     assert bool((whole[:len(lens)] == 77).all() and (whole[2 * len(lens):] == 77).all())
 
 
+def test_extend_into_the_most_rows_there_may_be():
+    """2^31 - 3 rows: the four of the last 16-byte store would end at row 2^31.  Rows behind the last are watched."""
+    n = (1 << 31) - 3
+    step = alloc_step(1, 0, "cuda")
+    step.positions, step.slots = (torch.full((n + 3,), 7, dtype=torch.int32, device="cuda") for _ in range(2))
+    whole = step.positions, step.slots
+    step.positions, step.slots = (t[:n] for t in whole)
+    rbs_paged_extend(_ints([0]), _ints([1]), _ints([[-1]]), _ints([0]), 1, 1, n, out=step)
+    assert step.lens.item() == 1 and step.cu.tolist() == [0, 1] and step.slots[0].item() == 0
+    assert whole[0][n:].tolist() == [7] * 3 and whole[1][n:].tolist() == [7] * 3
+    for part in range(0, n, 1 << 28):
+        assert not bool(step.positions[part:part + (1 << 28)].any()) and bool((step.slots[max(part, 1):part + (1 << 28)] == -1).all())
+
+
 def test_extend_step_after_step_hands_out_every_page_once():
     page, n_pages, seqs = 16, 61, 6
     g = np.random.default_rng(3)
