@@ -342,8 +342,8 @@ RBS_API rbs_status rbs_paged_extend(const rbs_paged_shape* shape, const int* seq
  *   pair i of rot_dim / 2 pairs, angle a_i = p * inv_freq[i]:
  *   (y_u, y_v) -> magnitude * (y_u cos a_i - y_v sin a_i,  y_v cos a_i + y_u sin a_i)
  *   with (u, v) = (i, i + rot_dim/2), or (2i, 2i + 1) if `interleaved`; elements from rot_dim on stay y.
- * fp32 arithmetic, one rounding to bf16 at the end; the angle is reduced in fp64, so far positions lose nothing.  Scaling for
- * long contexts is in inv_freq (any values) and magnitude. */
+ * fp32 arithmetic, one rounding to bf16 at the end.  The angle is off by 2^-26 of a revolution at any position, for frequencies of
+ * up to 2^40.  Scaling for long contexts is in inv_freq (any values) and magnitude. */
 typedef struct {
   const int* positions;    /* device, n_tokens ints; any sign */
   const float* inv_freq;   /* device, rot_dim / 2 floats (NULL if rot_dim == 0) */

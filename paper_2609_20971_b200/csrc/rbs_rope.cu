@@ -47,6 +47,7 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return d;
 }
 
+constexpr double kInvTwoPiLow = -9.839338337591243e-18;      // 1 / 2 pi - 0.15915494309189535
 // of a normal number
 __device__ __forceinline__ float fast_rsqrt(float x) {
   float y;
@@ -262,11 +263,13 @@ rope_kernel(const RopeParams p) {
   for (int i = 0; i < kRopeAhead; ++i) rows.fetch(open);
 
   // Angles in revolutions, as fractions of 2^64: positions are whole numbers, so whole revolutions of the frequency drop out of
-  // the product by themselves, and an angle is off by 2^-33 of a revolution at most however far the position is.
+  // the product by themselves.  The frequency is taken in two fp64 numbers (1 / 2 pi in 106 bits), off by 2^-64 of a revolution for
+  // frequencies up to 2^40, which a position makes 2^-33 at most.  What counts is the fp32 number of half revolutions in front
+  // of the sine: an angle is off by 2^-26 of a revolution, however far the position is.
   if (angle) {
-    double f = static_cast<double>(freq) * 0.15915494309189535;
-    f = (f - floor(f)) * 18446744073709551616.0;
-    const unsigned long long each = __double2ull_rn(f);
+    const double f = static_cast<double>(freq), high = f * 0.15915494309189535, low = fma(f, 0.15915494309189535, -high) + f * kInvTwoPiLow;
+    auto of_turn = [](double x) { return static_cast<unsigned long long>(__double2ll_rn((x - rint(x)) * 18446744073709551616.0)); };
+    const unsigned long long each = of_turn(high) + of_turn(low);
     for (int i = first;;) {
       float sn, cs;
       sincospif(static_cast<float>(static_cast<int>(static_cast<unsigned long long>(static_cast<long long>(pos)) * each >> 32)) *

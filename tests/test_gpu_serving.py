@@ -9,6 +9,7 @@ both and the fp32 sums.  lse: 1e-4 for the same reason."""
 import os
 import subprocess
 import sys
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -181,6 +182,30 @@ def test_angles_of_far_positions_are_exact():
     # the oracle's own angle, rounded to fp64, is off by up to 2^31 * 2^-53 = 2.4e-7: added to the 32 roundings of 6e-8
     want, size = so.norm_rope(_f64(q), pos.cpu().numpy(), _f64(freq))
     assert (np.abs(_f64(oq) - want) <= STEP * np.abs(want) + 40 * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_of_any_frequency_and_position(interleaved):
+    """Frequencies from 1e-6 to 2^40 of either sign, the angle in exact fractions with 60 digits of pi.  One element of each pair cancels to
+    less than 2^-12 of its two products, so that the result's rounding, 2^-20 of them, leaves the angle's error in sight.
+    Of their size, in 2^-24: angle 2^-25.9 revolutions 1.7, sine and cosine 2, magnitude 1, two products 2."""
+    pi = Fraction("3.14159265358979323846264338327950288419716939937510582097494")
+    freq = torch.tensor(np.geomspace(1e-6, 2.0 ** 40, 64) * (-1) ** (np.arange(64) // 5), dtype=torch.float32)
+    pos = [1, -1000, (1 << 24) + 1, 123456789, (1 << 31) - 1, -(1 << 31)]
+    turn = np.array([[float((p * Fraction(f) / (2 * pi)) % 1) for f in freq.tolist()] for p in pos])
+    cos, sin = np.cos(2 * np.pi * turn), np.sin(2 * np.pi * turn)
+    other = np.arange(128, 256)[:, None, None] / 128.0                     # every bf16 number of [1, 2) for v, and u beside it
+    u = torch.tensor(other * sin / cos).to(torch.bfloat16).double().numpy()
+    best = np.abs(u * cos / (other * sin) - 1).argmin(0)[None]
+    u, v = np.take_along_axis(u, best, 0)[0], other[best[0], 0, 0]
+    x = np.stack((u, v), -1 if interleaved else -2).reshape(len(pos), 1, 128)
+    q = torch.tensor(x, device="cuda").to(torch.bfloat16)
+    got = _f64(rbs_qk_norm_rope(q, q, _ints(pos), freq.cuda(), interleaved=interleaved)[0])
+    pairs = got.reshape(len(pos), 64, 2).transpose(2, 0, 1) if interleaved else got.reshape(len(pos), 2, 64).transpose(1, 0, 2)
+    for y, want in zip(pairs, (u * cos - v * sin, v * cos + u * sin)):
+        size = np.abs(u) + np.abs(v)
+        assert (np.abs(y - want) <= STEP * np.abs(want) + 8 * 2.0 ** -24 * size).all()
+    assert (np.abs(u * cos - v * sin) < 2.0 ** -12 * (np.abs(u) + np.abs(v))).all()
 
 
 def test_norm_of_zeros_and_of_small_and_large_rows():
