@@ -343,7 +343,7 @@ RBS_API rbs_status rbs_paged_extend(const rbs_paged_shape* shape, const int* seq
  *   (y_u, y_v) -> magnitude * (y_u cos a_i - y_v sin a_i,  y_v cos a_i + y_u sin a_i)
  *   with (u, v) = (i, i + rot_dim/2), or (2i, 2i + 1) if `interleaved`; elements from rot_dim on stay y.
  * fp32 arithmetic, one rounding to bf16 at the end.  The angle is off by 2^-26 of a revolution at any position, for frequencies of
- * up to 2^40.  Scaling for long contexts is in inv_freq (any values) and magnitude. */
+ * up to 2^40; an infinite frequency or a NaN gives NaN.  Scaling for long contexts is in inv_freq (any values) and magnitude. */
 typedef struct {
   const int* positions;    /* device, n_tokens ints; any sign */
   const float* inv_freq;   /* device, rot_dim / 2 floats (NULL if rot_dim == 0) */

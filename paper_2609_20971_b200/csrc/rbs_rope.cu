@@ -270,11 +270,12 @@ rope_kernel(const RopeParams p) {
     const double f = static_cast<double>(freq), high = f * 0.15915494309189535, low = fma(f, 0.15915494309189535, -high) + f * kInvTwoPiLow;
     auto of_turn = [](double x) { return static_cast<unsigned long long>(__double2ll_rn((x - rint(x)) * 18446744073709551616.0)); };
     const unsigned long long each = of_turn(high) + of_turn(low);
+    const float magnitude = fabsf(freq) <= 3.4028235e38f ? p.magnitude : __int_as_float(0x7fffffff);      // no angle, no result
     for (int i = first;;) {
       float sn, cs;
       sincospif(static_cast<float>(static_cast<int>(static_cast<unsigned long long>(static_cast<long long>(pos)) * each >> 32)) *
                     4.656612873077393e-10f, &sn, &cs);      // 2^-31: in half revolutions
-      angles[i][k] = make_float2(cs * p.magnitude, sn * p.magnitude);
+      angles[i][k] = make_float2(cs * magnitude, sn * magnitude);
       i += kRopeThreads / (kHeadDim / 2);
       if (i >= per_cta || token0 + i >= p.tokens) break;
       pos = position(i);

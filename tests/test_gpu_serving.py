@@ -208,6 +208,17 @@ def test_angles_of_any_frequency_and_position(interleaved):
     assert (np.abs(u * cos - v * sin) < 2.0 ** -12 * (np.abs(u) + np.abs(v))).all()
 
 
+def test_frequencies_that_are_no_numbers_give_no_numbers():
+    q, pos, freq = _randn(8, 5, 2, 128), torch.arange(5, dtype=torch.int32, device="cuda"), _frequencies(128)
+    clean, _ = rbs_qk_norm_rope(q, q, pos, freq)
+    freq[3], freq[10], freq[40] = float("inf"), float("nan"), -float("inf")
+    got, _ = rbs_qk_norm_rope(q, q, pos, freq)
+    bad = torch.tensor([i + 64 * j for i in (3, 10, 40) for j in (0, 1)], device="cuda")
+    assert bool(got[..., bad].isnan().all())
+    got[..., bad] = clean[..., bad]
+    assert torch.equal(got, clean)
+
+
 def test_norm_of_zeros_and_of_small_and_large_rows():
     q = _randn(7, 6, 2, 128)
     for row, scale in enumerate((0.0, 1e-12, 1e-18, 1e12, 3e17)):
