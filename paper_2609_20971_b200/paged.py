@@ -59,7 +59,8 @@ class PagedCache:
         self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=self.device)      # -1: no page
 
     def extend(self, new_lens: torch.Tensor, n_tokens: int) -> PagedStep:
-        """Room for new_lens[s] more tokens of each sequence, packed into n_tokens rows; their positions and slots."""
+        """Room for new_lens[s] more tokens of each sequence, packed into n_tokens rows; their positions and slots.  Tokens count in lens
+        whether or not there was a page for them: see short()."""
         n = self.lens.shape[0]
         state = torch.empty_like(self._state)
         out = PagedStep(state[:n], *(torch.empty(m, dtype=torch.int32, device=self.device) for m in (n + 1, n_tokens, n_tokens)), state[n:])
@@ -76,11 +77,19 @@ class PagedCache:
         """Attention of one token per sequence, Q [seqs, heads, d], over all that its sequence holds.  Keywords as rbs_paged_decode."""
         return rbs_paged_decode(Q, self.k[layer], self.v[layer], self.block_table, self.lens, **more)
 
-    def release(self, seqs) -> None:
-        """Ends sequences (a list of their rows): their pages become free.  Between steps, on the host's time: waits for the device."""
+    def short(self) -> list[int]:
+        """Sequences with tokens that got no page because the pool had run out.  Those tokens were not kept and `attend` leaves them out,
+        however many pages become free later: such a sequence has to be released and begun again.  Waits for the device."""
+        held = (self.lens.long() + self.page_size - 1) // self.page_size
+        missing = (self.block_table < 0) & (torch.arange(self.block_table.shape[1], device=self.device) < held[:, None])
+        return missing.any(1).nonzero()[:, 0].tolist()
+
+    def release(self, seqs) -> list[int]:
+        """Ends sequences (a list of their rows): their pages become free.  Between steps, on the host's time: waits for the device.
+        Returns what short() says of the sequences that go on."""
         ended = sorted(set(int(s) for s in seqs))
         if not ended:
-            return
+            return self.short()
         if ended[0] < 0 or ended[-1] >= self.lens.shape[0]:
             raise RbsError(f"PagedCache.release: sequences are 0 .. {self.lens.shape[0] - 1}")
         rows = torch.tensor(ended, dtype=torch.long, device=self.device)
@@ -94,3 +103,4 @@ class PagedCache:
         self.block_table[rows] = -1
         self.lens[rows] = 0
         self.used.zero_()
+        return self.short()

@@ -628,6 +628,17 @@ def test_prompts_and_generated_tokens_of_a_paged_cache():
         cache.release([3])
 
 
+def test_a_sequence_that_ran_out_of_pages_is_named_until_it_ends():
+    cache = PagedCache(1, 3, 16, 1, 2, 8, "cuda")
+    cache.extend(_ints([20, 10]), 30)
+    assert cache.short() == []
+    cache.extend(_ints([1, 9]), 10)                # the second one's 17th to 19th tokens find no page
+    assert cache.short() == [1] and cache.release([0]) == [1] and int(cache.used) == 0
+    step = cache.extend(_ints([0, 14]), 14)        # the page that is begun stays missing, the next one is there
+    assert (step.slots < 0).tolist() == [True] * 13 + [False] and cache.short() == [1]
+    assert cache.release([1]) == [] and int((cache.free_pages >= 0).sum()) == 3
+
+
 def test_calls_on_two_streams_at_once():
     """Two streams issue decode steps side by side, each with its own sequences; nothing is shared but the library."""
     streams = [torch.cuda.Stream() for _ in range(2)]

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from oracle import serving_oracle as so
-from paper_2609_20971_b200 import RbsError, binding, rbs_paged_decode, rbs_paged_extend, rbs_qk_norm_rope, rope_frequencies
+from paper_2609_20971_b200 import PagedCache, RbsError, binding, rbs_paged_decode, rbs_paged_extend, rbs_qk_norm_rope, rope_frequencies
 from paper_2609_20971_b200.binding import RbsPagedShape, RbsRope, RbsTensor
 
 OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
@@ -221,3 +221,16 @@ def test_rope_frequencies():
     for more in ({"scaling": "other"}, {"scaling": "yarn", "factor": 2.0}, {"factor": 0.5}):
         with pytest.raises(RbsError):
             rope_frequencies(64, 1e4, device="cpu", **more)
+
+
+def test_a_shortage_of_pages_can_be_seen_until_its_sequences_end():
+    """Three sequences on a pool of six pages: the second one's third page and the last one's only page were not there."""
+    cache = PagedCache(1, 6, 4, 1, 4, 5, "cpu")
+    cache.block_table[0, :2], cache.block_table[1, :2], cache.block_table[2, :2] = (torch.tensor(p, dtype=torch.int32) for p in ([4, 1], [0, 2], [5, 3]))
+    cache.lens.copy_(torch.tensor([8, 9, 5, 1]))
+    cache.used.fill_(8)
+    assert cache.short() == [1, 3]
+    assert cache.release([0]) == [1, 3] and int(cache.used) == 0      # pages are free again, tokens are still missing
+    assert cache.short() == [1, 3] and cache.release([]) == [1, 3]
+    assert cache.release([3]) == [1] and cache.release([1]) == []
+    assert sorted(cache.free_pages[cache.free_pages >= 0].tolist()) == [0, 1, 2, 4] and cache.lens.tolist() == [0, 0, 5, 0]
