@@ -36,8 +36,19 @@ def needs_build(lib: str = LIB) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def native_stamp() -> str | None:
+    """What the marshalling module is bound to; None where PyTorch is missing or has no CUDA, and the module cannot be built."""
+    try:
+        import torch
+    except ImportError:
+        return None
+    return f"torch {torch.__version__}, Python {sys.version_info.major}.{sys.version_info.minor}" if torch.version.cuda else None
+
+
 def build_native(force: bool = False) -> str:
     """Compiles the marshalling module with the host compiler against the installed PyTorch."""
+    if native_stamp() is None:
+        raise RuntimeError("the marshalling module of the serving calls needs a PyTorch with CUDA")
     deps = (NATIVE_SOURCE, os.path.join(ROOT, "include", "rbs.h"))
     if not force and os.path.exists(NATIVE) and all(os.path.getmtime(d) <= os.path.getmtime(NATIVE) for d in deps):
         return NATIVE
@@ -56,11 +67,13 @@ def build_native(force: bool = False) -> str:
 
 
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    """Compiles the sources (in parallel) and links the library; debug=True builds the checking variant."""
+    """Compiles the sources (in parallel) and links the library; debug=True builds the checking variant.  The marshalling module is built
+    along where the installed PyTorch allows; the library needs no PyTorch."""
     from concurrent.futures import ThreadPoolExecutor
 
     lib = LIB_DEBUG if debug else LIB
-    build_native(force)
+    if native_stamp() is not None:
+        build_native(force)
     if not force and not needs_build(lib):
         return lib
     suffix = ".debug.o" if debug else ".o"

@@ -234,3 +234,13 @@ def test_a_shortage_of_pages_can_be_seen_until_its_sequences_end():
     assert cache.short() == [1, 3] and cache.release([]) == [1, 3]
     assert cache.release([3]) == [1] and cache.release([1]) == []
     assert sorted(cache.free_pages[cache.free_pages >= 0].tolist()) == [0, 1, 2, 4] and cache.lens.tolist() == [0, 0, 5, 0]
+
+
+def test_the_library_builds_without_a_pytorch_with_cuda(lib, tmp_path, monkeypatch):
+    """Only the marshalling module needs one."""
+    from paper_2609_20971_b200 import build
+    monkeypatch.setattr(build, "NATIVE", str(tmp_path / "_native.so"))
+    monkeypatch.setattr(torch.version, "cuda", None)
+    assert build.build_library() == build.LIB and not (tmp_path / "_native.so").exists()
+    with pytest.raises(RuntimeError):
+        build.build_native()
