@@ -14,6 +14,7 @@ SOURCES = ["rbs_api.cu", "rbs_tmap.cu", "rbs_stats.cu", "rbs_select.cu", "rbs_pr
            "rbs_extend.cu", "rbs_rope.cu", "rbs_decode.cu"]
 NATIVE = os.path.join(PKG, "_native.so")                # marshalling of PyTorch's tensors, see csrc/rbs_torch.cpp
 NATIVE_SOURCE = os.path.join(CSRC, "rbs_torch.cpp")
+NATIVE_STAMP = os.path.join(PKG, "_native.stamp")       # the PyTorch and the Python that it was built against
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -45,12 +46,21 @@ def native_stamp() -> str | None:
     return f"torch {torch.__version__}, Python {sys.version_info.major}.{sys.version_info.minor}" if torch.version.cuda else None
 
 
+def needs_native() -> bool:
+    """Whether the module is missing, older than its source, or built against another PyTorch or Python."""
+    deps = (NATIVE_SOURCE, os.path.join(ROOT, "include", "rbs.h"))
+    if not os.path.exists(NATIVE) or not os.path.exists(NATIVE_STAMP) or any(os.path.getmtime(d) > os.path.getmtime(NATIVE) for d in deps):
+        return True
+    with open(NATIVE_STAMP) as f:
+        return f.read() != native_stamp()
+
+
 def build_native(force: bool = False) -> str:
     """Compiles the marshalling module with the host compiler against the installed PyTorch."""
-    if native_stamp() is None:
+    stamp = native_stamp()
+    if stamp is None:
         raise RuntimeError("the marshalling module of the serving calls needs a PyTorch with CUDA")
-    deps = (NATIVE_SOURCE, os.path.join(ROOT, "include", "rbs.h"))
-    if not force and os.path.exists(NATIVE) and all(os.path.getmtime(d) <= os.path.getmtime(NATIVE) for d in deps):
+    if not force and not needs_native():
         return NATIVE
     import sysconfig
 
@@ -63,6 +73,8 @@ def build_native(force: bool = False) -> str:
                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
                     *(x for p in system for x in ("-isystem", p)), NATIVE_SOURCE, "-o", NATIVE, "-L", os.path.join(base, "lib"),
                     "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"], check=True)
+    with open(NATIVE_STAMP, "w") as f:
+        f.write(stamp)
     return NATIVE
 
 

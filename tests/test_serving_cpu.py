@@ -240,7 +240,20 @@ def test_the_library_builds_without_a_pytorch_with_cuda(lib, tmp_path, monkeypat
     """Only the marshalling module needs one."""
     from paper_2609_20971_b200 import build
     monkeypatch.setattr(build, "NATIVE", str(tmp_path / "_native.so"))
+    monkeypatch.setattr(build, "NATIVE_STAMP", str(tmp_path / "_native.stamp"))
     monkeypatch.setattr(torch.version, "cuda", None)
     assert build.build_library() == build.LIB and not (tmp_path / "_native.so").exists()
     with pytest.raises(RuntimeError):
         build.build_native()
+
+
+def test_the_marshalling_module_is_rebuilt_for_another_pytorch(lib, tmp_path, monkeypatch):
+    from paper_2609_20971_b200 import build
+    assert not build.needs_native()
+    stamp = tmp_path / "_native.stamp"
+    monkeypatch.setattr(build, "NATIVE_STAMP", str(stamp))
+    assert build.needs_native()
+    stamp.write_text(build.native_stamp())
+    assert not build.needs_native()
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    assert build.needs_native()
