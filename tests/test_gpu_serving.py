@@ -16,7 +16,7 @@ import pytest
 import torch
 
 from oracle import serving_oracle as so
-from paper_2609_20971_b200 import (PagedCache, RbsError, alloc_step, paged_decode_workspace_bytes, rbs_device_status, rbs_paged_decode,
+from paper_2609_20971_b200 import (PagedCache, PagedStep, RbsError, alloc_step, paged_decode_workspace_bytes, rbs_device_status, rbs_paged_decode,
                                    rbs_paged_extend, rbs_qk_norm_rope, rbs_qk_norm_rope_paged, rope_frequencies)
 from paper_2609_20971_b200.binding import rbs_prefill_varlen
 
@@ -79,6 +79,39 @@ def test_extend_equals_the_oracle(seed, seqs, page, most, old, new, n_free, n_pa
             assert np.array_equal(x, y), name
         assert out.used.item() == want[5]
     assert bool((whole[:, most:] == 77).all())
+
+
+def _many_rows(seed, page, rows, pool):
+    """Zeros and lengths of 1 to 3 beside long ones, 200,000 to 260,000 tokens; `rows` more rows than tokens, `pool` more pages than needed."""
+    g = np.random.default_rng(seed)
+    seqs = 700
+    add = np.where(g.random(seqs) < 0.03, g.integers(8000, 13000, seqs), g.integers(0, 4, seqs))
+    add[:5], add[100:110], add[-3:] = 0, 0, 0
+    add[300] += 210000 - add.sum() if add.sum() < 210000 else 0
+    lens = g.integers(0, 3 * page + 2, seqs)
+    most = int((-(-(lens + add) // page)).max()) + 1
+    need = int((-(-(lens + add) // page) + -lens // page).sum())
+    n_pages = int((-(-lens // page)).sum()) + need + 10
+    return lens, add, g.integers(0, n_pages, (seqs, most)), g.permutation(n_pages)[:need + pool], 0, page, n_pages, int(add.sum()) + rows
+
+
+MANY_ROWS = [(1, 1, 0, 5), (2, 16, 1, 5), (3, 24, 6, 5), (4, 16, -20000, 5), (5, 24, 3, -700), (6, 1, -3333, -100000)]
+
+
+@pytest.mark.parametrize("seed, page, rows, pool", MANY_ROWS)
+@pytest.mark.parametrize("offset", [0, 1])      # outputs that take 16-byte stores, and that do not
+def test_extend_of_many_rows_equals_the_oracle(seed, page, rows, pool, offset):
+    lens, add, table, free, used, page, n_pages, tokens = _many_rows(seed, page, rows, pool)
+    assert tokens > 1024 * torch.cuda.get_device_properties(0).multi_processor_count
+    want = so.extend(lens, add, table, free, page, n_pages, tokens, used)
+    whole = [torch.full((n + 9,), -99, dtype=torch.int32, device="cuda") for n in (len(lens), len(lens) + 1, tokens, tokens, 1)]
+    out = PagedStep(*(t[offset:t.shape[0] - 9 + offset] for t in whole))
+    rows = _ints(table)
+    rbs_paged_extend(_ints(lens), _ints(add), rows, _ints(free), page, n_pages, tokens, free_used=_ints([used]), out=out)
+    for x, y in zip((rows, out.lens, out.cu, out.positions, out.slots), want):
+        assert np.array_equal(x.cpu().numpy(), y)
+    assert out.used.item() == want[5]
+    assert all(bool((t[:offset] == -99).all() and (t[t.shape[0] - 9 + offset:] == -99).all()) for t in whole)
 
 
 @pytest.mark.parametrize("lens, add, page, most", [
@@ -171,6 +204,20 @@ def test_norm_rope_of_a_batch_in_place_and_with_one_norm_only():
     assert oq is q and ok is k and torch.equal(apart[0], q) and torch.equal(apart[1], k)
     _check_turn(q, q0, pos, freq, None)
     _check_turn(k, k0, pos, freq, w)
+
+
+# 2, 4 and 8 tokens to a thread block, blocks that begin in one entry of the batch and end in another one or in the fourth
+@pytest.mark.parametrize("batch, tokens, hq, hkv", [(3, 301, 3, 1), (5, 401, 2, 1), (7, 701, 4, 2), (1000, 3, 2, 1), (2600, 1, 1, 1)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_norm_rope_of_large_batches_equals_the_oracle(batch, tokens, hq, hkv, interleaved):
+    x = _randn(batch, tokens, batch, hq + hkv, 128, scale=2.0).transpose(0, 1)      # the batch is not the slowest dimension
+    q, k = x.split((hq, hkv), dim=2)
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    pos = torch.randint(0, 1 << 18, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    freq, w = _frequencies(96), torch.randn(128, generator=g, device="cuda")
+    oq, ok = rbs_qk_norm_rope(q, k, pos, freq, q_norm=w, eps=1e-5, interleaved=interleaved)
+    _check_turn(oq, q, pos, freq, w, eps=1e-5, interleaved=interleaved)
+    _check_turn(ok, k, pos, freq, None, interleaved=interleaved)
 
 
 def test_angles_of_far_positions_are_exact():
@@ -390,6 +437,34 @@ def test_decode_of_sequences_that_share_their_pages():
     assert sum(-(-n // 16) + 2 for n in lens) > 444 * 4 * 32
     out, lse = rbs_paged_decode(q, k, v, table, _ints(lens), return_lse=True)
     _check_decode(out, lse, q, k, v, table, _ints(lens))
+
+
+def _shared(seed, seqs, hq, hkv, page, longest):
+    """Block tables that all name the same pages, and lengths with work for two waves of thread blocks."""
+    k, v, table, _ = _sequences(seed, [longest], page, hkv)
+    lens = [longest - 7 * (i % 40) for i in range(seqs)]
+    items = hkv * (-(-(hq // hkv) // 16))
+    assert sum(-(-n // 16) + 2 for n in lens) * items > 444 * 4 * 32
+    return _randn(seed + 1, seqs, hq, 128, scale=1.5), k, v, table.expand(seqs, -1).contiguous(), _ints(lens)
+
+
+SHARED = [(31, 330, 3, 1, 24, 2900), (32, 330, 9, 1, 16, 2900), (33, 330, 16, 1, 24, 2900), (34, 110, 40, 1, 16, 3000), (35, 100, 16, 4, 16, 2600),
+          (36, 100, 64, 4, 24, 2600)]
+
+
+@pytest.mark.parametrize("seed, seqs, hq, hkv, page, longest", SHARED)
+def test_decode_in_two_waves(seed, seqs, hq, hkv, page, longest):
+    q, k, v, table, lens = _shared(seed, seqs, hq, hkv, page, longest)
+    out, lse = rbs_paged_decode(q, k, v, table, lens, return_lse=True)
+    t = torch.arange(longest, device="cuda")
+    kd, vd = (x[table[0, t // page].long(), t % page].double().transpose(0, 1) for x in (k, v))      # [hkv, tokens, 128]
+    score = q.double().view(seqs, hkv, hq // hkv, 128).transpose(0, 1) @ kd.transpose(1, 2)[:, None] / 128 ** 0.5
+    score.masked_fill_(t >= lens[:, None, None], -torch.inf)
+    p = score.softmax(-1)
+    ref, size = ((p @ x[:, None]).transpose(0, 1).reshape(seqs, hq, 128) for x in (vd, vd.abs()))
+    assert bool(((out.double() - ref).abs() <= STEP * ref.abs() + (2.0 ** -16 + 1e-4) * size).all())
+    assert float((lse.double() - score.logsumexp(-1).transpose(0, 1).reshape(seqs, hq)).abs().max()) <= 1e-4
+    assert torch.equal(out, rbs_paged_decode(q, k, v, table, lens))
 
 
 def test_decode_leaves_out_tokens_whose_page_does_not_exist():
@@ -725,3 +800,26 @@ def test_debug_library_runs_the_calls_clean_and_bit_identical(tmp_path):
     r = subprocess.run([sys.executable, "-c", DEBUG_CHILD, str(tmp_path / "out.pt")], env=env, cwd=root, capture_output=True, text=True, timeout=600)
     assert r.returncode == 0 and "debug child ok" in r.stdout, r.stdout[-2000:] + r.stderr[-4000:]
     assert all(torch.equal(x, y) for x, y in zip(torch.load(tmp_path / "out.pt"), debug_outputs(), strict=True))
+
+
+def debug_outputs_of_large_calls():
+    got = []
+    for case in SHARED:
+        got += rbs_paged_decode(*_shared(*case), return_lse=True)
+    for case in MANY_ROWS:
+        lens, add, table, free, used, page, n_pages, tokens = _many_rows(*case)
+        table = _ints(table)
+        out = rbs_paged_extend(_ints(lens), _ints(add), table, _ints(free), page, n_pages, tokens, free_used=_ints([used]))
+        got += [table, out.lens, out.cu, out.positions, out.slots, out.used]
+    return [x.cpu() for x in got]
+
+
+def test_debug_library_runs_large_calls_clean_and_bit_identical(tmp_path):
+    from paper_2609_20971_b200.build import build_library
+    build_library(debug=True)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = dict(os.environ, RBS_DEBUG="1", PYTHONPATH=root + os.pathsep + os.environ.get("PYTHONPATH", ""))
+    child = DEBUG_CHILD.replace("debug_outputs()", "debug_outputs_of_large_calls()")
+    r = subprocess.run([sys.executable, "-c", child, str(tmp_path / "out.pt")], env=env, cwd=root, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0 and "debug child ok" in r.stdout, r.stdout[-2000:] + r.stderr[-4000:]
+    assert all(torch.equal(x, y) for x, y in zip(torch.load(tmp_path / "out.pt"), debug_outputs_of_large_calls(), strict=True))
