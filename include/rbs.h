@@ -383,9 +383,10 @@ RBS_API rbs_status rbs_qk_norm_rope_paged(const rbs_paged_shape* shape, int n_to
  * Q, O: row s = sequence s (stride_token, stride_head; stride_batch ignored); O may be Q itself (same pointer and strides).  bf16
  * inputs, fp32 accumulation and softmax, bf16 output.  n_s is taken into [0, max_pages*page_size]; tokens whose page lies outside [0, n_pages) are left out.
  * A sequence without a token gets zeros and lse = -inf.  lse (nullable): fp32 [S][Hq], natural-log-sum-exp of the scaled logits.
- * softmax_scale == 0 means 1/sqrt(d).  The work of all sequences is cut into equal pieces on the device (no
- * length is read on the host, so a captured graph follows them); a sequence that is cut is joined in a fixed order: a call
- * with the same lengths gives the same bits, a sequence in another batch agrees to rounding.
+ * softmax_scale == 0 means 1/sqrt(d); it may be negative, and |softmax_scale * log2(e)| must be finite in fp32.  The work of all
+ * sequences is cut into equal pieces on the device (no length is read on the host, so a captured graph follows them); a
+ * sequence that is cut is joined in a fixed order: a call with the same lengths gives the same bits, a sequence in another
+ * batch agrees to rounding.
  * Workspace: rbs_paged_decode_workspace_bytes(shape) bytes, 256-byte aligned (its size depends on the group size alone); calls that
  * may run at the same time need one each.
  * RBS_ERR_UNSUPPORTED where the table could hold 2^31 tiles of 16 tokens and more over all sequences and KV heads.

@@ -872,7 +872,7 @@ extern "C" rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor 
   NvtxRange range("rbs_paged_decode");
   rbs_status st = check_paged_table(shape);
   if (st != RBS_OK || (st = check_paged_cache(shape)) != RBS_OK) return st;
-  if (block_table == nullptr || seq_lens == nullptr || !(fabsf(softmax_scale) <= 3.4028235e38f)) return RBS_ERR_INVALID_ARG;
+  if (block_table == nullptr || seq_lens == nullptr || !(fabsf(softmax_scale * kLog2e) <= 3.4028235e38f)) return RBS_ERR_INVALID_ARG;
   Q.stride_batch = O.stride_batch = 0;
   if ((st = check_tensor(Q)) != RBS_OK || (st = check_tensor(O)) != RBS_OK || (st = check_tensor(k_cache)) != RBS_OK ||
       (st = check_tensor(v_cache)) != RBS_OK)

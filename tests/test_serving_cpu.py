@@ -140,6 +140,11 @@ def test_decode_refuses_arguments(lib, args):
     assert _decode(lib, _shape(), **args) == INVALID
 
 
+@pytest.mark.parametrize("scale", [3e38, -2.4e38])
+def test_decode_refuses_scales_that_are_infinite_in_units_of_log_2(lib, scale):
+    assert _decode(lib, _shape(), scale=scale) == INVALID
+
+
 def test_decode_refuses_tables_of_too_many_tiles(lib):
     big = dict(n_seqs=1 << 13, n_q_heads=64, n_kv_heads=64, max_pages=1 << 17, table_stride=1 << 17)
     assert _decode(lib, _shape(**big)) == UNSUPPORTED
