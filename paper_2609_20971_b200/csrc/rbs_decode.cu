@@ -59,6 +59,10 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
 __device__ __forceinline__ uint32_t bf16_below(float x) {
   return static_cast<uint32_t>(max(__float_as_int(x) - 0x8000, 0)) & 0xffff0000u;
 }
+// x += y of two neighbouring numbers, in one instruction
+__device__ __forceinline__ void add_pair(float* x, const float* y) {
+  f2_unpack(f2_add(f2_pack(x[0], x[1]), f2_pack(y[0], y[1])), x[0], x[1]);
+}
 // The value that exponentials are taken against: nothing seen yet must not give inf - inf.
 __device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (exp_base(m) + log2f(l)) * 0.6931471805599453f; }
@@ -119,7 +123,7 @@ struct Softmax {
 #pragma unroll
     for (int n = 0; n < HT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) c[n][i] += c2[n][i];
+      for (int i = 0; i < 4; i += 2) add_pair(c[n] + i, c2[n] + i);
     const bool lo = (valid >> g) & 1, hi = (valid >> (g + 8)) & 1;
     bool move = false;
 #pragma unroll
@@ -168,8 +172,9 @@ struct Softmax {
   // 2-norm, 64 sequences of 64 heads: two bf16 numbers and one running sum 1.2e-4 (207.9 us), three numbers the same (210.2),
   // with tiles summed by themselves 3.9e-5 (212.7), with the scores' product in two sums as well 2.9e-5 (212.9); plain fp32
   // operations 5.8e-5.
-  // Products of kSide x 16 elements go side by side, because the three of a sum wait for each other: 17 sequences with pages of 24
-  // 16.75 -> 16.25 us, 64 sequences of 128 heads in groups of 16 255 -> 245 (221 with two numbers and one running sum).
+  // Products of four times 16 elements go side by side, because the three of a sum wait for each other: 17 sequences with pages of 24
+  // 16.75 -> 16.25 us, 64 sequences of 128 heads in groups of 16 272 -> 257 (232 with two numbers and one running sum: there the
+  // products and their instructions count, not HBM).
   __device__ __forceinline__ void values(uint32_t vtile, const float (&c)[HT][4]) {
     const int lane = threadIdx.x & 31;
     uint32_t p[HT][6];
@@ -187,7 +192,7 @@ struct Softmax {
         }
         p[n][4 + i] = transpose_8x8(pack_bf16(x, y));
       }
-    constexpr int kSide = HT == 1 ? 4 : 2;
+    constexpr int kSide = 4;
 #pragma unroll
     for (int j = 0; j < 8; j += kSide) {
       uint32_t a[kSide][4];
@@ -206,7 +211,7 @@ struct Softmax {
 #pragma unroll
         for (int n = 0; n < HT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[n][j + b][i] += sum[b][n][i];
+          for (int i = 0; i < 4; i += 2) add_pair(o[n][j + b] + i, sum[b][n] + i);
     }
   }
 
