@@ -359,7 +359,8 @@ typedef struct {
  * Q_out, K_out = norm and rotation of Q [batch][n_tokens][n_q_heads][128] and K [batch][n_tokens][n_kv_heads][128], whose
  * tokens have the positions rope->positions (the same for every batch entry).  One launch.  An output may be its own input
  * (same pointer and strides); it must not overlap an input in another way, nor itself (a batch stride of 0 is
- * RBS_ERR_INVALID_ARG for the outputs of a batch).  Head counts: any positive ones.
+ * RBS_ERR_INVALID_ARG for the outputs of a batch).  Batch, n_tokens and head counts: any positive ones (0 is RBS_ERR_INVALID_ARG
+ * here, in the paged form and in the prefill calls; of the serving calls only rbs_paged_extend has a use for n_tokens == 0).
  */
 RBS_API rbs_status rbs_qk_norm_rope(int batch, int n_tokens, int n_q_heads, int n_kv_heads, int head_dim, rbs_tensor Q,
                                     rbs_tensor K, const rbs_rope* rope, rbs_tensor Q_out, rbs_tensor K_out, void* stream);

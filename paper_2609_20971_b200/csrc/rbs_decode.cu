@@ -1,7 +1,9 @@
 // rbs_paged_decode: attention of one new token per sequence over a paged key/value cache.
 // One pass over the keys and values with the running maximum and sum of the softmax.  The cache is read once: 512 bytes per
-// token and KV head against 4 * 128 * G operations, far below what either kind of unit can do, so HBM is the bound and all
-// else is arranged to keep loads in flight.
+// token and KV head against 4 * 128 * G operations, far below what either kind of unit can do, so HBM is the bound for groups of up
+// to 8 heads (64 sequences of 64 heads: 211 us, 6.5 TB/s) and all else is arranged to keep loads in flight.  With 16 heads to
+// a KV head the products of a warp take longer than its loads (257 us for the same bytes); larger groups are cut, and
+// each cut reads the cache anew (32 heads: 65 us where 16 take 40).
 //
 // The work of all sequences stands in one order -- sequence by sequence, item by item (KV head, cut of its query heads), tile by
 // tile of 16 tokens -- and is cut into equal shares, one per warp, whatever the lengths are.  A warp works alone: its own
@@ -371,9 +373,9 @@ struct TileSource {
 };
 
 // Shares are cut in units of work: the tiles of an item, and behind them kDecItemCost for its end (in all fewer than 2^31).  The
-// first wave of CTAs gets equal shares.  CTAs do not end together, though: SMs differ in what they get of the memory
-// (128K tokens: ends between 45 and 57 us).  So large calls leave a tenth to a second wave of smaller shares, which the first
-// CTAs to end make room for: 64 sequences of 64 heads 217 -> 210 us.  In smaller ones their start costs more than that.
+// first wave of CTAs gets equal shares.  CTAs do not end together, though: SMs differ in what they get of the memory.  So large
+// calls leave a tenth to a second wave of smaller shares, which the first CTAs to end make room for: 64 sequences of 64 heads
+// 229 -> 213 us.  In smaller ones their start costs more than that.
 struct Cuts {
   unsigned total, first;              // units; those of the first wave
   unsigned ctas, wave;                // CTAs with a share; those of the first wave
@@ -761,7 +763,7 @@ constexpr int kJoinThreads = 256;
 // their way together; the groups are joined in order, maxima first.  The order depends on the lengths alone.
 // It becomes resident at the end of the kernel above, and lets no later kernel do so before its own end: the kernel above fills
 // every SM exactly, and where waiting CTAs had taken places of its own its last CTAs started late (64 sequences of 64 heads:
-// 239 us instead of 218 with triggers at both kernels' begins).
+// 224 us instead of 213 with triggers at both kernels' begins).
 template <int HT>
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const DecodeParams p) {

@@ -2,7 +2,8 @@
 // Whole numbers only.  With c the prefix sums of the new lengths (cut at the rows there are) and
 //   first_s = ceil(past_s / P),  last_s = ceil((past_s + c_{s+1} - c_s) / P),  a_s = prefix sums of last_s - first_s
 // page p of sequence s, first_s <= p < last_s, is entry free_used + a_s + p - first_s of the free list.
-// Bound by its launch: a decode step of 64 sequences moves 2 KB, half a million prompt tokens 4.8 MB.
+// A decode step of 64 sequences moves 2 KB and is bound by its launch (2.8 us); 1.2 million prompt tokens move 9.6 MB and are bound by
+// the scan in front of their stores (8.1 us).
 #include "rbs_common.cuh"
 #include "rbs_sm100.cuh"
 
@@ -81,7 +82,7 @@ __device__ __forceinline__ int last_not_above(const int* a, int n, int v) {
 
 // Every CTA scans all lengths for itself (from L2, into shared memory), so that nothing is handed from CTA to CTA; then the
 // CTAs share out the sequences, the new table entries and the token rows.  One CTA per SM and 16-byte stores where there are many
-// rows (1.2 million rows of 301 prompts: 8.0 us, of which the scan 2.5; two CTAs per SM 10.3; eight rows one after the other, whose
+// rows (1.2 million rows of 301 prompts: 8.1 us, of which the scan 2.5; two CTAs per SM 10.3; eight rows one after the other, whose
 // stores leave gaps, 8.7); one row per thread otherwise (a decode step of 64 sequences: 2.8 us, 4.9 with eight).
 template <int THREADS, int ROWS, int GROUPS>
 __global__ void __launch_bounds__(THREADS)

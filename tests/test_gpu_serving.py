@@ -3,9 +3,8 @@
 Tolerances (a bf16 rounding is off by at most 2^-8 of the value).
 Norm and rotation: one rounding of the result, 2^-8 |r|; in front of it some twenty fp32 roundings of the two products a result
 is the difference of, 32 * 2^-24 of their sizes.
-Decode: the result's rounding, 2^-8 |o|; the probabilities, held in two bf16 numbers, 2^-16 sum(p |v|); fp32 scores of at most
-|q||k| scale ~ 40 summed over 128 products are off by about 1e-5 and their exponentials by as much, 1e-4 of sum(p |v|) covers
-both and the fp32 sums.  lse: 1e-4 for the same reason."""
+Decode: the result's rounding, 2^-8 |o|; the probabilities, 2^-16 sum(p |v|); fp32 scores of at most |q||k| scale ~ 40 summed
+over 128 products are off by about 1e-5 and their exponentials by as much, 1e-4 of sum(p |v|) covers both and the fp32 sums.  lse: 1e-4 for the same reason."""
 import os
 import subprocess
 import sys
