@@ -439,8 +439,8 @@ RBS_API rbs_status rbs_paged_read_int4(const rbs_paged_shape* shape, rbs_cache_i
  * exist, cut sequences, repeated calls), with
  *   O_s = sum_{t < n_s} softmax_t(q_s.k_t * scale) v_t
  * over the numbers that the cache stands for.  Products see keys and values exactly; queries are rounded to 2^-25 of the largest element
- * of their head; sums and maxima have 32 bits.  Probabilities are rounded to fp16 (2^-11 of each) for their product with the values, not for
- * their sum and lse: an element of O is off by 2^-11 of sum(p |v|) beside its own rounding to bf16.
+ * of their head; sums and maxima have 32 bits.  Probabilities enter their product with the values as two numbers that keep 22 bits of
+ * them (and 2^-36 of the largest); their sum and lse take them as they are.
  * Workspace: rbs_paged_decode_int4_workspace_bytes(shape) bytes, 256-byte aligned (its size depends on the group size alone).
  * RBS_ERR_UNSUPPORTED where the table could hold 2^31 tiles of 32 tokens and more over all sequences and KV heads.
  */

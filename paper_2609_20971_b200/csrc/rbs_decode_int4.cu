@@ -7,6 +7,7 @@
 //   - rows are stored in their natural order; the elements of a row that meet in a step of the product over the head, and the
 //     tokens that meet in a step of the product over the tokens, are chosen so that a lane finds all of its bits in 16 (keys)
 //     or 8 (values) bytes in a row.
+//   - a probability is two fp16 numbers of 11 bits each.
 #include "rbs_decode.cuh"
 #include "rbs_int4.cuh"
 
@@ -295,20 +296,24 @@ struct Softmax4 {
       }
   }
 
-  // Adds P V of a tile.  Probabilities go into the product as fp16 numbers, off by at most 2^-11 of themselves (2^-25, which is 2^-36 of
-  // the largest probability, where that is more), while their sum l keeps them as they are: an element of the output is off by up to
-  // 2^-11 of sum(p |v|), against the 2^-8 of its own rounding.  (With a second fp16 number for what is left: 95 us instead of 84 for 64
-  // sequences of 64 heads, and the same error of the output: 1.7e-3 of its norm either way.)  The sums of the product drop bits in
-  // one direction, so a tile is summed from zero and added by itself.
+  // Adds P V of a tile.  A probability of up to 2^15 goes into the product as two fp16 numbers, its first 11 bits and what is left, to 2^-22
+  // of it (2^-25 at the least, which is 2^-36 of the largest probability).  One number takes 81 us instead of 92 (64 sequences of 64 heads),
+  // but leaves values that cancel 11 bits, and outputs differ from those of 32-bit operations by 6e-4 of their norm instead of 6e-5.
+  // The sums of the product drop bits in one direction, so a tile is summed from zero, the small parts first, and added by itself.
   __device__ __forceinline__ void values(uint32_t tile, const float (&c)[2][HT][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    uint32_t p[2][HT][2];      // of the halves of the tile
+    uint32_t p[2][2][HT][2];      // half of the tile; what is left, first bits
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int n = 0; n < HT; ++n)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) p[h][n][i] = transpose_8x8(pack_half(c[h][n][2 * i], c[h][n][2 * i + 1]));
+        for (int i = 0; i < 2; ++i) {
+          const float x = c[h][n][2 * i], y = c[h][n][2 * i + 1];
+          const float fx = __uint_as_float(__float_as_uint(x) & 0xffffe000u), fy = __uint_as_float(__float_as_uint(y) & 0xffffe000u);
+          p[h][1][n][i] = transpose_8x8(pack_half(fx, fy));
+          p[h][0][n][i] = transpose_8x8(pack_half(x - fx, y - fy));
+        }
     // tokens t, 4 + (t ^ 1) and those eight further on; elements 16 g .. 16 g + 15
     const int other = 4 + (t ^ 1);
     const uint32_t chunk = (((g >> 1) ^ (t & 2)) << 4) + ((g & 1) << 3);
@@ -337,14 +342,16 @@ struct Softmax4 {
         v[h][1][0] = x[2]; v[h][1][1] = x[3]; v[h][1][2] = y[2]; v[h][1][3] = y[3];
       }
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int part = 0; part < 2; ++part)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int n = 0; n < HT; ++n) {
-            if (h == 0) mma_f16_16816_zero(sum[j][n], v[h][j], p[h][n][0], p[h][n][1]);
-            else mma_f16_16816(sum[j][n], v[h][j], p[h][n][0], p[h][n][1]);
-          }
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int n = 0; n < HT; ++n) {
+              if (part == 0 && h == 0) mma_f16_16816_zero(sum[j][n], v[h][j], p[h][part][n][0], p[h][part][n][1]);
+              else mma_f16_16816(sum[j][n], v[h][j], p[h][part][n][0], p[h][part][n][1]);
+            }
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
