@@ -477,7 +477,8 @@ struct Source {
   __device__ __forceinline__ uint32_t copy_runs(const Decode4Params& p, uint32_t tile) const {
     const int lane = threadIdx.x & 31, r = lane >> 2 & 3;      // row of the half, less a multiple of 4
     const bool there = page >= 0 && page < p.n_pages;
-    const uint32_t in = there ? page : 0, at64 = offset * 64u, at8 = offset * 8u;
+    const uint32_t in = there ? page : 0;
+    const uint64_t row64 = static_cast<uint32_t>(offset), at64 = row64 * 64, at8 = row64 * 8;      // beyond 32 bits in pages of 2^26 tokens and more
     // a 32-bit number times a 64-bit one
     auto from = [&](const unsigned char* base, int64_t stride) { return base + in * static_cast<uint64_t>(stride); };
     const unsigned char *from_k = from(k, p.kp) + at64, *from_v = from(v, p.vp) + at64, *from_ks = from(ks, p.ksp) + at8, *from_vs = from(vs, p.vsp) + at8;
