@@ -135,7 +135,7 @@ __device__ __forceinline__ int token_of(int k) { return (k & 8) | (k & 1 ? 4 + (
 // ------------------------------------------------------------------------------------------------ queries
 
 // Q^T of up to 8 * HT heads, the B operand of the eight steps over the head dimension: lane (g, t) has elements 32 t .. 32 t + 31 of heads
-// 8 n + g.  In fp16 they are multiples of 2^-25 or less of the head's largest element, which is brought to [1, 2).
+// 8 n + g.  In fp16 they are off by at most 2^-25 of the head's largest element, which is brought to [1, 2).
 template <int HT>
 struct Queries4 {
   uint4 raw[HT][4];      // bf16, as they are loaded
@@ -163,10 +163,14 @@ struct Queries4 {
       uint32_t most = max(top & 0xffffu, top >> 16);
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      const uint32_t power = min(max(most >> 7, 1u), 253u);      // 127 + the exponent of the largest
-      // a negative scale goes into the queries; a scale is never zero, which the scores of keys that are left out would not stand
-      const float down = __uint_as_float((254u - power) << 23 | (__float_as_uint(scale_log2) & 0x80000000u));
-      const float up = fmaxf(__uint_as_float(power << 23) * (fabsf(scale_log2) * kValueScale), 0x1p-126f);
+      const int power = max(127 - static_cast<int>(most >> 7), -126);      // minus the exponent of the largest
+      // a negative scale goes into the queries
+      const float down = __uint_as_float(static_cast<uint32_t>(127 + power) << 23 | (__float_as_uint(scale_log2) & 0x80000000u));
+      // kValueScale |scale| / 2^power: what its parts make beyond 32 bits must not make it infinite, nor anything make it zero, which the
+      // scores of zero and the scores of keys that are left out would not stand
+      const int half = power / 2;
+      const float halves[2] = {__uint_as_float(static_cast<uint32_t>(127 - half) << 23), __uint_as_float(static_cast<uint32_t>(127 + half - power) << 23)};
+      const float up = fminf(fmaxf(fabsf(scale_log2) * halves[0] * kValueScale * halves[1], 0x1p-126f), 3.4028235e38f);
       scale[n][0] = __shfl_sync(0xffffffffu, up, 8 * t);
       scale[n][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4);
 #pragma unroll
