@@ -135,7 +135,9 @@ __device__ __forceinline__ int token_of(int k) { return (k & 8) | (k & 1 ? 4 + (
 // ------------------------------------------------------------------------------------------------ queries
 
 // Q^T of up to 8 * HT heads, the B operand of the eight steps over the head dimension: lane (g, t) has elements 32 t .. 32 t + 31 of heads
-// 8 n + g.  In fp16 they are off by at most 2^-25 of the head's largest element, which is brought to [1, 2).
+// 8 n + g, in fp16 and times the power of two that brings the head's largest element to [2^14, 2^15) (at most 2^127, which leaves
+// subnormal ones between 2^-6 and 2).  So bf16 numbers of down to 2^-31 of the largest keep all of their bits and smaller ones are off by up to
+// 2^-39 of it; sums of 128 products with keys of up to 8 * 480 / kValueScale stay below 2^31.
 template <int HT>
 struct Queries4 {
   uint4 raw[HT][4];      // bf16, as they are loaded
@@ -163,7 +165,7 @@ struct Queries4 {
       uint32_t most = max(top & 0xffffu, top >> 16);
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      const int power = max(127 - static_cast<int>(most >> 7), -126);      // minus the exponent of the largest
+      const int power = min(141 - static_cast<int>(most >> 7), 127);      // 14 less the exponent of the largest
       // a negative scale goes into the queries
       const float down = __uint_as_float(static_cast<uint32_t>(127 + power) << 23 | (__float_as_uint(scale_log2) & 0x80000000u));
       // kValueScale |scale| / 2^power: what its parts make beyond 32 bits must not make it infinite, nor anything make it zero, which the
