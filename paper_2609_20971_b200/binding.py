@@ -591,6 +591,13 @@ def rbs_paged_write_int4(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, 
     (_native or load_native()).paged_write_int4(K, V, slots, *k_cache, *v_cache)
 
 
+def _qk_norm_rope_write_int4(Q, K, V, positions, slots, inv_freq, k_cache, v_cache, *, q_norm=None, k_norm=None, eps=1e-6, interleaved=False,
+                             magnitude=1.0, out_q=None, out_k=None):
+    """rbs_qk_norm_rope and rbs_paged_write_int4 of its keys, refused as one call.  Returns Q'."""
+    return (_native or load_native()).qk_norm_rope_write_int4(Q, K, V, positions, inv_freq, q_norm, k_norm, eps, interleaved, magnitude, slots, *k_cache,
+                                                              *v_cache, out_q, out_k)
+
+
 def rbs_paged_read_int4(k_cache, v_cache, block_table: torch.Tensor, cu_rows: torch.Tensor, n_rows: int, *, starts: torch.Tensor | None = None,
                         out_k: torch.Tensor | None = None, out_v: torch.Tensor | None = None):
     """What sequences hold, as bf16 rows K, V [n_rows, kv_heads, 128] for the prefill calls, exactly: rows cu_rows[s] .. cu_rows[s + 1] - 1 are

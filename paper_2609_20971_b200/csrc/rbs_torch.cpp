@@ -151,6 +151,11 @@ class Call {
     r.magnitude = number(i + 6);
     return r;
   }
+  // what the library asks of rows, for a call that launches something before it asks
+  void on_borders(const rbs_tensor& t) const {
+    if (reinterpret_cast<uintptr_t>(t.ptr) % 16 != 0 || t.stride_token <= 0 || t.stride_head <= 0 || t.stride_token % 8 != 0 || t.stride_head % 8 != 0)
+      refuse("expected rows on 16-byte borders, positive multiples of 8 elements apart");
+  }
   at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type) const {
     return at::detail::empty_cuda(sizes, type, c10::Device(c10::kCUDA, static_cast<c10::DeviceIndex>(device_)), std::nullopt);
   }
@@ -356,6 +361,36 @@ PyObject* write_int4(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// Q, K, V, positions, inv_freq, q_norm, k_norm, eps, interleaved, magnitude, slots, k codes, k scales, v codes, v scales, out_q, out_k:
+// norm_rope and write_int4 of its keys.  All that either refuses is refused before the first one has changed anything.
+PyObject* norm_rope_write_int4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Call c("norm, rotation and rbs_paged_write_int4", args, n, 17);
+    const at::Tensor &q = c.tensor(0), &k = c.tensor(1), &v = c.tensor(2), &slots = c.tensor(10);
+    if (q.dim() != 3) c.refuse("Q must be [tokens, heads, 128]");
+    const int64_t tokens = q.size(0), d = q.size(2);
+    rbs_paged_shape shape = {};
+    const rbs_cache_int4 kc = c.cache_int4(11, d, shape), vc = c.cache_int4(13, d, shape);
+    shape.n_seqs = shape.max_pages = shape.table_stride = 1;
+    shape.n_q_heads = shape.n_kv_heads;
+    const int64_t kv[3] = {tokens, shape.n_kv_heads, d};
+    const rbs_rope rope = c.rope(3, tokens, d);
+    if (slots.numel() > tokens) c.refuse("more slots than tokens");
+    const rbs_tensor tq = c.rows(q, q.sizes()), tk = c.rows(k, kv), tv = c.rows(v, kv);
+    const at::Tensor out_q = c.output(15, q), out_k = c.output(16, k);
+    const rbs_tensor oq = c.rows(out_q, q.sizes()), ok = c.rows(out_k, kv);
+    const int* s = c.vector<int>(slots, slots.numel());
+    c.on_borders(tv);
+    c.run([&](void* stream) {
+      rbs_status st = lib_write_int4(&shape, 0, ok, tv, s, kc, vc, stream);      // checks the caches
+      if (st == RBS_OK) st = lib_norm_rope(1, c.small(tokens), c.small(q.size(1)), shape.n_kv_heads, c.small(d), tq, tk, &rope, oq, ok, stream);
+      if (st == RBS_OK) st = lib_write_int4(&shape, c.small(slots.numel()), ok, tv, s, kc, vc, stream);
+      return st;
+    });
+    return THPVariable_Wrap(out_q);
+  });
+}
+
 // k codes, k scales, v codes, v scales, block_table, cu_rows, n_rows, starts, out_k, out_v
 PyObject* read_int4(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -439,6 +474,7 @@ PyMethodDef methods[] = {{"bind", method(bind), METH_FASTCALL, nullptr},
                          {"qk_norm_rope_paged", method(norm_rope_paged), METH_FASTCALL, nullptr},
                          {"paged_decode", method(decode), METH_FASTCALL, nullptr},
                          {"paged_write_int4", method(write_int4), METH_FASTCALL, nullptr},
+                         {"qk_norm_rope_write_int4", method(norm_rope_write_int4), METH_FASTCALL, nullptr},
                          {"paged_read_int4", method(read_int4), METH_FASTCALL, nullptr},
                          {"paged_decode_int4", method(decode_int4), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -11,8 +11,8 @@ import math
 
 import torch
 
-from .binding import (PagedStep, RbsError, rbs_paged_decode, rbs_paged_decode_int4, rbs_paged_extend, rbs_paged_read_int4, rbs_paged_write_int4,
-                      rbs_qk_norm_rope, rbs_qk_norm_rope_paged)
+from .binding import (PagedStep, RbsError, _qk_norm_rope_write_int4, rbs_paged_decode, rbs_paged_decode_int4, rbs_paged_extend, rbs_paged_read_int4,
+                      rbs_qk_norm_rope_paged)
 
 
 def rope_frequencies(rot_dim: int, base: float, *, scaling: str | None = None, factor: float = 1.0, trained_len: int = 0, fast: float = 32.0,
@@ -84,13 +84,10 @@ class PagedCache:
         return out
 
     def write(self, layer: int, Q, K, V, step: PagedStep, inv_freq, **turn):
-        """Norms and rotates Q, K of the tokens of `step` and keeps K and V.  Returns Q (and K, if out_k is given).  Keywords as
+        """Norms and rotates Q, K of the tokens of `step` and keeps K and V.  Returns Q'; out_k, if given, receives K' too.  Keywords as
         rbs_qk_norm_rope_paged."""
-        if self.bits == 16:
-            return rbs_qk_norm_rope_paged(Q, K, V, step.positions, step.slots, inv_freq, *self._layer(layer), **turn)
-        Q, K = rbs_qk_norm_rope(Q, K, step.positions, inv_freq, **turn)
-        rbs_paged_write_int4(K, V, step.slots, *self._layer(layer))
-        return Q
+        call = rbs_qk_norm_rope_paged if self.bits == 16 else _qk_norm_rope_write_int4
+        return call(Q, K, V, step.positions, step.slots, inv_freq, *self._layer(layer), **turn)
 
     def attend(self, layer: int, Q, **more):
         """Attention of one token per sequence, Q [seqs, heads, d], over all that its sequence holds.  Keywords as rbs_paged_decode."""
