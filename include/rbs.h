@@ -390,7 +390,8 @@ RBS_API rbs_status rbs_qk_norm_rope_paged(const rbs_paged_shape* shape, int n_to
  * batch agrees to rounding.
  * Workspace: rbs_paged_decode_workspace_bytes(shape) bytes, 256-byte aligned (its size depends on the group size alone); calls that
  * may run at the same time need one each.
- * RBS_ERR_UNSUPPORTED where the table could hold 2^31 tiles of 16 tokens and more over all sequences and KV heads.
+ * RBS_ERR_UNSUPPORTED: 2^24 query heads and more; tables that could hold 2^31 - 1 units of work and more, which are max_pages*page_size / 16 + 3 for
+ * every sequence, KV head and started 16 query heads of a group.
  */
 RBS_API size_t rbs_paged_decode_workspace_bytes(const rbs_paged_shape* shape);
 RBS_API rbs_status rbs_paged_decode(const rbs_paged_shape* shape, rbs_tensor Q, rbs_tensor k_cache, rbs_tensor v_cache,
@@ -443,7 +444,8 @@ RBS_API rbs_status rbs_paged_read_int4(const rbs_paged_shape* shape, rbs_cache_i
  * values as two numbers that keep 22 bits of them (and 2^-36 of the largest); their sum and lse take them as they are.  Scores have to be
  * finite in 32 bits in units of log 2.
  * Workspace: rbs_paged_decode_int4_workspace_bytes(shape) bytes, 256-byte aligned (its size depends on the group size alone).
- * RBS_ERR_UNSUPPORTED where the table could hold 2^31 tiles of 32 tokens and more over all sequences and KV heads.
+ * RBS_ERR_UNSUPPORTED: 2^24 query heads and more; tables that could hold 2^31 - 1 units of work and more, which are max_pages*page_size / 32 + 3 for
+ * every sequence, KV head and started 16 query heads of a group.
  */
 RBS_API size_t rbs_paged_decode_int4_workspace_bytes(const rbs_paged_shape* shape);
 RBS_API rbs_status rbs_paged_decode_int4(const rbs_paged_shape* shape, rbs_tensor Q, rbs_cache_int4 k_cache, rbs_cache_int4 v_cache,

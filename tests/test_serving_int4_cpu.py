@@ -117,6 +117,22 @@ def test_decode_refuses_tables_of_too_many_tiles_and_workspaces(lib):
         assert _decode(lib, **args) == WORKSPACE
 
 
+@pytest.mark.parametrize("keys", [16, 32])
+def test_decode_takes_tables_up_to_the_border_of_31_bits(lib, keys):
+    """A call that is taken goes on to the workspace, which is refused here."""
+    def call(**change):
+        s = _shape(n_seqs=1, table_stride=1 << 20, **change)
+        if keys == 32:
+            return _decode(lib, s, ws=None)
+        return lib.rbs_paged_decode(s, _t(), _t(), _t(), P, P, _t(), None, 0.0, None, 0, None)
+    heads = 1 << 16
+    for hq, hkv in ((heads, heads), (heads * 16, heads), (heads // 2 * 17, heads // 2), (heads // 2 * 32, heads // 2)):
+        for units, want in ((32767, WORKSPACE), (32768, UNSUPPORTED)):      # 2^16 of them, of which 3 are not for tokens
+            assert call(n_q_heads=hq, n_kv_heads=hkv, page_size=keys, max_pages=units - 3) == want
+    assert call(n_q_heads=15 << 20, n_kv_heads=1 << 20, max_pages=1) == WORKSPACE
+    assert call(n_q_heads=1 << 24, n_kv_heads=1 << 20, max_pages=1) == UNSUPPORTED
+
+
 def test_calls_refuse_host_tensors_and_caches_of_other_bits():
     x, ints = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
     cache = torch.zeros(3, 16, 4, 64, dtype=torch.uint8), torch.zeros(3, 16, 4, 8, dtype=torch.uint8)
