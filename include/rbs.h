@@ -441,7 +441,7 @@ RBS_API rbs_status rbs_paged_read_int4(const rbs_paged_shape* shape, rbs_cache_i
  *   O_s = sum_{t < n_s} softmax_t(q_s.k_t * scale) v_t
  * over the numbers that the cache stands for.  Products see keys and values exactly, and queries but for elements below 2^-31 of the
  * largest of their head, which are off by up to 2^-39 of it; sums and maxima have 32 bits.  Probabilities enter their product with the
- * values as two numbers that keep 22 bits of them (and 2^-36 of the largest); their sum and lse take them as they are.  Scores have to be
+ * values as two numbers that keep 22 bits of them (and 2^-35 of the largest); their sum and lse take them as they are.  Scores have to be
  * finite in 32 bits in units of log 2.
  * Workspace: rbs_paged_decode_int4_workspace_bytes(shape) bytes, 256-byte aligned (its size depends on the group size alone).
  * RBS_ERR_UNSUPPORTED: 2^24 query heads and more; tables that could hold 2^31 - 1 units of work and more, which are max_pages*page_size / 32 + 3 for

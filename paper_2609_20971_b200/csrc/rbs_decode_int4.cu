@@ -303,7 +303,7 @@ struct Softmax4 {
   }
 
   // Adds P V of a tile.  A probability of up to 2^15 goes into the product as two fp16 numbers, its first 11 bits and what is left, to 2^-22
-  // of it (2^-25 at the least, which is 2^-36 of the largest probability).  One number takes 81 us instead of 92 (64 sequences of 64 heads),
+  // of it (2^-24 at the least, which is 2^-35 of the largest probability).  One number takes 81 us instead of 92 (64 sequences of 64 heads),
   // but leaves values that cancel 11 bits, and outputs differ from those of 32-bit operations by 6e-4 of their norm instead of 6e-5.
   // The sums of the product drop bits in one direction, so a tile is summed from zero, the small parts first, and added by itself.
   __device__ __forceinline__ void values(uint32_t tile, const float (&c)[2][HT][4]) {
@@ -562,7 +562,7 @@ decode_int4_kernel(const Decode4Params p) {
     int s = at.s, hk = at.hk, cut = at.cut, item = at.item;      // the item that is summed
     bool begun_here = at.tile == 0, finished = false;
 
-    // tiles i + 1 and i + 2 are on their way while tile i is worked on, the table entries of tile i + 3 as well
+    // tile i + 1 is on its way while tile i is worked on, the table entries of tile i + 2 as well
     source.end = share.end;
     source.item(p);
     uint32_t valid[kStages4];
